@@ -293,6 +293,74 @@ st3_status st3_prefill_attend_kept(const void* q, const void* k, const void* v, 
 st3_status st3_attend_noalloc(const void* q, const void* k, const void* v, void* out, int32_t num_heads,
                               int32_t num_rows, int32_t head_dim, int32_t dtype, void* cuda_stream);
 
+/* ---- A cache of grouped heads held in 8 bits -----------------------------------------------------------------------
+ *
+ * One layer's keys and values, with the tokens' positions and the attention weight they have accumulated.  Rows
+ * 0 .. held-1 of a (sequence, head) are in use, in any order; how many is an argument of each call.  A block is 64 rows;
+ * row r has the values code * scale[r / 64].  The scale is a power of two 2^e, -60 <= e <= 60, the smallest with
+ * max|x| <= 127 * 2^e over the block: values are then exact in bf16, and a block whose scale grows is moved to
+ * it by one rounding of its codes.  Values beyond 127 * 2^60 are clamped; NaN and Inf are stored as 0 and reported as
+ * ST3_DEV_NONFINITE.  All arrays are dense, owned by the caller, aligned to 16 bytes. */
+typedef struct {
+  int32_t batch, num_kv_heads;
+  int32_t head_dim;      /* 64 or 128                                                     */
+  int32_t capacity;      /* rows per (sequence, head), a multiple of 64                   */
+  int8_t* k;             /* dev [batch][num_kv_heads][capacity][head_dim]                 */
+  int8_t* v;
+  float* k_scale;        /* dev [batch][num_kv_heads][capacity / 64]                      */
+  float* v_scale;
+  int32_t* ids;          /* dev [batch][num_kv_heads][capacity]: position of each row     */
+  float* weights;        /* dev [batch][num_kv_heads][capacity]: accumulated weight       */
+} st3_cache;
+
+/* Stores the rows cu[s] .. cu[s+1]-1 of k and v (dtype ST3_F32 or ST3_BF16; strides in elements from one token and
+ * one head to the next, multiples of 16 bytes, the elements of a head side by side) as rows start[s],
+ * start[s]+1, ... of sequence s, with the positions pos[s], pos[s]+1, ... and weight 0: a prompt, a piece of one, or the
+ * new token of a decode step.
+ *   total       rows of k and v in all
+ *   start       dev int32 [batch]: rows held before the call (NULL: 0)
+ *   pos         dev int32 [batch] (NULL: start)
+ *   dev_status  dev int, may be NULL.  Rows that would leave the cache or the tensors: ST3_DEV_RANGE, the sequence is
+ *               skipped. */
+st3_status st3_cache_store(const st3_cache* cache, const void* k, const void* v, int32_t dtype, int64_t k_token_stride,
+                           int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int32_t* cu,
+                           int32_t total, const int32_t* start, const int32_t* pos, int* dev_status, void* cuda_stream);
+
+/* One query per head over the rows held (Eq. 2, last row), query head h on key/value head h / (num_heads / num_kv_heads).
+ *   q, out       dev [batch][num_heads][head_dim], dtype
+ *   held         dev int32 [batch], 0 allowed (the output is then 0); above the capacity: ST3_DEV_RANGE, cut to it
+ *   weights_out  dev fp32 [batch][num_kv_heads][capacity] or NULL: weights_in plus each held row's probability, summed over the
+ *                heads of its group; may be weights_in (and is, for accumulation in the cache).  Other rows are left as
+ *                they were.
+ *   workspace    dev, aligned to 256 bytes, of at least st3_cache_attend_workspace's size (with_weights: whether calls
+ *                will pass weights_out); calls that may run at the same time need one each */
+st3_status st3_cache_attend_workspace(const st3_cache* cache, int32_t num_heads, int32_t with_weights, size_t* bytes);
+st3_status st3_cache_attend(const st3_cache* cache, const void* q, void* out, int32_t dtype, int32_t num_heads,
+                            const int32_t* held, const float* weights_in, float* weights_out, void* workspace,
+                            size_t bytes, int* dev_status, void* cuda_stream);
+
+/* Cuts every (sequence, head) that holds more than `keep` rows to `keep`: the rows of the last `recent` positions (those
+ * >= seen[s] - recent) stay, and of the others the ones with the largest accumulated weight, ties toward the earlier
+ * position.  The kept rows below the new length stay where they are; the holes among them, from the first on, get the
+ * kept rows from behind it, in their order.  A block that receives a row gets the scale of the rows it then holds.
+ *   to           where the result goes: `from` itself (in place: blocks without a hole are not touched) or another
+ *                cache with the same batch, heads and head_dim and room for `keep` rows
+ *   held         dev int32 [batch] rows held now
+ *   seen         dev int32 [batch] tokens the sequence has seen, i.e. the position of its next token
+ *   held_out     dev int32 [batch] min(held, keep); may be held
+ *   recent       0 <= recent <= keep; keep >= 1.  Positions within a head are distinct.
+ * A weight that is NaN counts as the lowest and sets ST3_DEV_NONFINITE. */
+st3_status st3_cache_evict_workspace(const st3_cache* from, size_t* bytes);
+st3_status st3_cache_evict(const st3_cache* from, const st3_cache* to, const int32_t* held, const int32_t* seen,
+                           int32_t keep, int32_t recent, int32_t* held_out, void* workspace, size_t bytes,
+                           int* dev_status, void* cuda_stream);
+
+/* Reads rows first[s] .. first[s] + num_rows - 1 of every (sequence, head) back as values: k, v (dev
+ * [batch][num_kv_heads][num_rows][head_dim], dtype), ids and weights (dev [batch][num_kv_heads][num_rows]).  Any of the
+ * four may be NULL; first NULL: 0.  Rows that are not held read as 0. */
+st3_status st3_cache_rows(const st3_cache* cache, const int32_t* first, const int32_t* held, int32_t num_rows, void* k,
+                          void* v, int32_t dtype, int32_t* ids, float* weights, void* cuda_stream);
+
 const char* st3_status_string(st3_status s);
 
 /* Frees the host-side context.  Does not synchronise and does not touch the workspace. */

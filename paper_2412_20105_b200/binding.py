@@ -24,7 +24,9 @@ EXPORTS = ["st3_schedule_count", "st3_workspace_size", "st3_create", "st3_prefil
            "st3_prefill_select_scored", "st3_decode_step",
            "st3_decode_step_host", "st3_prefill_select_host", "st3_host_sync", "st3_get_kept", "st3_get_rows", "st3_get_status", "st3_rows_held",
            "st3_set_overlap", "st3_profile_enable", "st3_profile_read", "st3_launch_count", "st3_status_string", "st3_destroy",
-           "st3_attend_noalloc", "st3_prefill_attend", "st3_prefill_attend_kept"]
+           "st3_attend_noalloc", "st3_prefill_attend", "st3_prefill_attend_kept",
+           "st3_cache_store", "st3_cache_attend_workspace", "st3_cache_attend", "st3_cache_evict_workspace",
+           "st3_cache_evict", "st3_cache_rows"]
 
 
 class Config(C.Structure):
@@ -33,6 +35,12 @@ class Config(C.Structure):
         "num_layers", "num_heads", "head_dim", "dtype", "batch", "sys_len", "num_visual", "max_text_len",
         "max_decode_steps", "first_prune_layer", "stride", "first_ratio_bp", "step_ratio_bp", "anneal",
         "disable_trim", "rows_per_chunk", "static_rank", "stage_shared", "host_prefill")] + [("lazy_mask", C.c_uint64), ("tau", C.c_double), ("sigma", C.c_double)]
+
+
+class CacheDesc(C.Structure):
+    """Mirror of `st3_cache` (include/st3.h)."""
+    _fields_ = [(n, C.c_int32) for n in ("batch", "num_kv_heads", "head_dim", "capacity")] + [
+        (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "ids", "weights")]
 
 
 class St3Error(RuntimeError):
@@ -82,6 +90,13 @@ def load():
     lib.st3_attend_noalloc.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
     lib.st3_prefill_attend.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]
     lib.st3_prefill_attend_kept.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, i32, vp]
+    cp, szp = C.POINTER(CacheDesc), C.POINTER(C.c_size_t)
+    lib.st3_cache_store.argtypes = [cp, vp, vp, i32, i64, i64, i64, i64, vp, i32, vp, vp, vp, vp]
+    lib.st3_cache_attend_workspace.argtypes = [cp, i32, i32, szp]
+    lib.st3_cache_attend.argtypes = [cp, vp, vp, i32, i32, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    lib.st3_cache_evict_workspace.argtypes = [cp, szp]
+    lib.st3_cache_evict.argtypes = [cp, cp, vp, vp, i32, i32, vp, vp, C.c_size_t, vp, vp]
+    lib.st3_cache_rows.argtypes = [cp, vp, vp, i32, vp, vp, i32, vp, vp, vp]
     for name in EXPORTS:
         if name not in ("st3_schedule_count", "st3_launch_count", "st3_status_string"):
             getattr(lib, name).restype = C.c_int
@@ -229,6 +244,175 @@ def st3_attend_noalloc(q, k, v, out, num_heads, num_rows, head_dim, dtype, strea
     the size limit and the sharing rules)."""
     dt = {"f32": ST3_F32, "bf16": ST3_BF16}.get(dtype, dtype)
     _check(load().st3_attend_noalloc(q, k, v, out, num_heads, num_rows, head_dim, dt, stream), "st3_attend_noalloc")
+
+
+def st3_cache_store(cache, k, v, dtype, k_strides, v_strides, cu, total, start=None, pos=None, dev_status=None, stream=0):
+    """cache is a CacheDesc; k_strides and v_strides are (token, head) strides in elements; the rest device addresses."""
+    _check(load().st3_cache_store(C.byref(cache), k, v, dtype, *k_strides, *v_strides, cu, total, start, pos, dev_status,
+                                  stream), "st3_cache_store")
+
+
+def st3_cache_attend_workspace(cache, num_heads, with_weights) -> int:
+    n = C.c_size_t(0)
+    _check(load().st3_cache_attend_workspace(C.byref(cache), num_heads, int(with_weights), C.byref(n)),
+           "st3_cache_attend_workspace")
+    return n.value
+
+
+def st3_cache_attend(cache, q, out, dtype, num_heads, held, weights_in, weights_out, workspace, nbytes, dev_status=None,
+                     stream=0):
+    _check(load().st3_cache_attend(C.byref(cache), q, out, dtype, num_heads, held, weights_in, weights_out, workspace,
+                                   nbytes, dev_status, stream), "st3_cache_attend")
+
+
+def st3_cache_evict_workspace(cache) -> int:
+    n = C.c_size_t(0)
+    _check(load().st3_cache_evict_workspace(C.byref(cache), C.byref(n)), "st3_cache_evict_workspace")
+    return n.value
+
+
+def st3_cache_evict(cache, to, held, seen, keep, recent, held_out, workspace, nbytes, dev_status=None, stream=0):
+    _check(load().st3_cache_evict(C.byref(cache), C.byref(to), held, seen, keep, recent, held_out, workspace, nbytes,
+                                  dev_status, stream), "st3_cache_evict")
+
+
+def st3_cache_rows(cache, first, held, num_rows, k, v, dtype, ids, weights, stream=0):
+    _check(load().st3_cache_rows(C.byref(cache), first, held, num_rows, k, v, dtype, ids, weights, stream),
+           "st3_cache_rows")
+
+
+_DTYPES = {}     # torch dtype -> st3_dtype
+
+
+def _dtype_of(t) -> int:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: ST3_BF16, torch.float32: ST3_F32})
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"bfloat16 or float32 is needed, not {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _stream_of(t) -> int:
+    """The current stream of the tensor's device, which has to be the current device."""
+    import torch
+    index = t.device.index
+    if not t.is_cuda or index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _dense(t, shape, dtype, device, what):
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of {tuple(shape)} on {device} is needed, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows_view(t, heads, dim, dtype, device, what):
+    """Address and (token, head) strides of a [tokens, heads, dim] tensor whose last dimension is dense."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{what}: a {dtype} tensor of [tokens, {heads}, {dim}] on {device} is needed, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.stride(2) != 1:
+        raise ValueError(f"{what}: the elements of a head have to lie side by side")
+    return t.data_ptr(), (t.stride(0), t.stride(1))
+
+
+class Cache:
+    """One layer's cache of grouped heads held in 8 bits (st3_cache), over tensors of the caller's or its own.
+
+    `Cache(k, v, k_scale, v_scale, ids, weights)` wraps existing tensors, `Cache.empty(...)` allocates them.  `status` is
+    the device status word that the calls report into.  How many rows each sequence holds is the caller's to keep: an
+    int32 tensor [batch] that goes into the calls.  The workspaces are kept between calls: use a Cache on one stream
+    at a time."""
+
+    def __init__(self, k, v, k_scale, v_scale, ids, weights):
+        import torch
+        n, heads, cap, dim = k.shape
+        if not k.is_cuda:
+            raise ValueError("a CUDA device is required: this library has no CPU path")
+        self.torch, self.device = torch, k.device
+        self.k, self.v, self.k_scale, self.v_scale, self.ids, self.weights = k, v, k_scale, v_scale, ids, weights
+        codes, blocks = (n, heads, cap, dim), (n, heads, cap // 64)
+        f32, i32 = torch.float32, torch.int32
+        self.desc = CacheDesc(n, heads, dim, cap, _dense(k, codes, torch.int8, k.device, "k"),
+                              _dense(v, codes, torch.int8, k.device, "v"), _dense(k_scale, blocks, f32, k.device, "k_scale"),
+                              _dense(v_scale, blocks, f32, k.device, "v_scale"), _dense(ids, codes[:3], i32, k.device, "ids"),
+                              _dense(weights, codes[:3], f32, k.device, "weights"))
+        self.batch, self.num_kv_heads, self.capacity, self.head_dim = n, heads, cap, dim
+        self.status = torch.zeros(1, dtype=i32, device=k.device)
+        self._attend_ws = self._evict_ws = None
+        self._attend_bytes = {}
+
+    @classmethod
+    def empty(cls, batch, num_kv_heads, head_dim, capacity, device="cuda:0"):
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("a CUDA device is required: this library has no CPU path")
+        cap = (capacity + 63) // 64 * 64
+        new = functools.partial(torch.empty, device=device)
+        codes = (batch, num_kv_heads, cap, head_dim)
+        return cls(new(codes, dtype=torch.int8), new(codes, dtype=torch.int8), new(*codes[:2], cap // 64),
+                   new(*codes[:2], cap // 64), new(codes[:3], dtype=torch.int32), new(codes[:3]))
+
+    def _count(self, t, what):
+        return None if t is None else _dense(t, (self.batch,), self.torch.int32, self.device, what)
+
+    def _workspace(self, ws, nbytes):
+        if ws is None or ws.numel() < nbytes + 256:
+            ws = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
+        return ws, (ws.data_ptr() + 255) // 256 * 256
+
+    def store(self, k, v, cu, start=None, pos=None):
+        """Rows cu[s] .. cu[s+1]-1 of k and v ([tokens, kv heads, dim]) go behind the start[s] rows of sequence s."""
+        dt = _dtype_of(k)
+        kp, ks = _rows_view(k, self.num_kv_heads, self.head_dim, k.dtype, self.device, "k")
+        vp, vs = _rows_view(v, self.num_kv_heads, self.head_dim, k.dtype, self.device, "v")
+        if v.shape[0] != k.shape[0]:
+            raise ValueError("k and v have different numbers of rows")
+        st3_cache_store(self.desc, kp, vp, dt, ks, vs, _dense(cu, (self.batch + 1,), self.torch.int32, self.device, "cu"),
+                        k.shape[0], self._count(start, "start"), self._count(pos, "pos"), self.status.data_ptr(),
+                        _stream_of(k))
+
+    def attend(self, q, held, out, weights_out=None, weights_in=None):
+        """q and out [batch, heads, dim]; weights_out (e.g. this cache's `weights`) gets weights_in (None: this cache's)
+        plus the probabilities."""
+        heads, dt = q.shape[1], _dtype_of(q)
+        shape = (self.batch, heads, self.head_dim)
+        wi = wo = None
+        if weights_out is not None:
+            wi = _dense(self.weights if weights_in is None else weights_in, self.weights.shape, self.torch.float32, self.device, "weights_in")
+            wo = _dense(weights_out, self.weights.shape, self.torch.float32, self.device, "weights_out")
+        key = (heads, wo is not None)
+        if key not in self._attend_bytes:
+            self._attend_bytes[key] = st3_cache_attend_workspace(self.desc, *key)
+        self._attend_ws, ws = self._workspace(self._attend_ws, self._attend_bytes[key])
+        st3_cache_attend(self.desc, _dense(q, shape, q.dtype, self.device, "q"), _dense(out, shape, q.dtype, self.device, "out"),
+                         dt, heads, self._count(held, "held"), wi, wo, ws, self._attend_bytes[key], self.status.data_ptr(),
+                         _stream_of(q))
+
+    def evict(self, held, seen, keep, recent=0, into=None, held_out=None):
+        """Cuts every head to `keep` rows, in place or into another Cache; returns the new numbers of rows held."""
+        to = self if into is None else into
+        if held_out is None:
+            held_out = self.torch.empty_like(held)
+        if self._evict_ws is None:
+            self._evict_bytes = st3_cache_evict_workspace(self.desc)
+        self._evict_ws, ws = self._workspace(self._evict_ws, self._evict_bytes)
+        st3_cache_evict(self.desc, to.desc, self._count(held, "held"), self._count(seen, "seen"), keep, recent,
+                        self._count(held_out, "held_out"), ws, self._evict_bytes, self.status.data_ptr(), _stream_of(held))
+        return held_out
+
+    def rows(self, held, num_rows, first=None, dtype=None):
+        """(k, v, ids, weights) of rows first[s] .. first[s] + num_rows - 1 as values; rows that are not held read as 0."""
+        t = self.torch
+        shape = (self.batch, self.num_kv_heads, num_rows)
+        k, v = (t.empty(shape + (self.head_dim,), dtype=dtype or t.bfloat16, device=self.device) for _ in range(2))
+        ids, weights = t.empty(shape, dtype=t.int32, device=self.device), t.empty(shape, device=self.device)
+        st3_cache_rows(self.desc, self._count(first, "first"), self._count(held, "held"), num_rows, k.data_ptr(),
+                       v.data_ptr(), _dtype_of(k), ids.data_ptr(), weights.data_ptr(), _stream_of(k))
+        return k, v, ids, weights
 
 
 class Context:

@@ -1,0 +1,747 @@
+// A key/value cache of grouped heads held in 8 bits: rows in, one query over it, eviction by accumulated weight, rows out.
+//
+// A block is 64 rows of one (sequence, head); its values are code * 2^e with the smallest e, -60 <= e <= 60, for which the
+// block's largest magnitude is at most 127 * 2^e.  A power of two costs half a bit of the codes on average against a
+// free scale.  It buys: no division (x * 2^-e is exact, the only rounding is that to a code); values that are exact in
+// bf16; and a block whose scale grows, because a row was appended or moved in, is moved to the new scale by one
+// rounding, or by none where the scale stays, so that rows which move often do not wear out.
+//
+// Every kernel here may be set up while the launch ahead of it runs (programmatic dependent launch) and waits for it
+// before the first access to memory, in every block.
+#include "st3_common.cuh"
+
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include "st3_launch.cuh"
+
+namespace {
+
+constexpr int kBlockRows = 64;
+constexpr int kMaxExp = 60;
+
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2i(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
+// log2 of a scale; whatever a caller's array holds, the result stays in the range of scales
+__device__ __forceinline__ int scale_exp(float s) {
+  const int e = (int)((__float_as_uint(s) >> 23) & 0xffu) - 127;
+  return min(max(e, -kMaxExp), kMaxExp);
+}
+// The smallest e in [-60, 60] with amax <= 127 * 2^e: 1.m * 2^x <= 127/64 * 2^(e + 6).
+__device__ __forceinline__ int block_exp(float amax) {
+  const unsigned b = __float_as_uint(amax);
+  const int e = (int)(b >> 23) - 133 + ((b & 0x7fffffu) > 0x7e0000u);
+  return min(max(e, -kMaxExp), kMaxExp);
+}
+__device__ __forceinline__ int code_of(float x, float inv_scale) {   // half to even
+  return (int)fminf(fmaxf(rintf(x * inv_scale), -127.f), 127.f);
+}
+__device__ __forceinline__ unsigned pack4(int a, int b, int c, int d) {
+  return (unsigned)(a & 0xff) | ((unsigned)(b & 0xff) << 8) | ((unsigned)(c & 0xff) << 16) | ((unsigned)d << 24);
+}
+__device__ __forceinline__ int byte_of(unsigned w, int i) { return (int)(signed char)(w >> (8 * i)); }
+__device__ __forceinline__ int clamp_rows(int n, int cap) { return min(max(n, 0), cap); }
+
+struct CacheView {
+  int8_t* code[2];       // k, v
+  float* scale[2];
+  int* ids;
+  float* weights;
+  int batch, heads, cap;
+};
+
+// ------------------------------------------------------------------------------------------------------------------
+// Rows in.  One thread block per (64-row block that receives rows, head, K or V).
+// ------------------------------------------------------------------------------------------------------------------
+struct StoreParams {
+  CacheView c;
+  const void* src[2];
+  long long token_stride[2], head_stride[2];
+  const int* cu;
+  const int* start;
+  const int* pos;
+  int* status;
+  int total;
+};
+
+constexpr int kStoreThreads = 256;
+
+// 8 elements of a row as floats, with what is not finite as 0 (and noted in `bad`)
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&f)[8], bool& bad) {
+  if constexpr (sizeof(T) == 2) {
+    unpack16(*reinterpret_cast<const uint4*>(p), f);
+  } else {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (!(fabsf(f[i]) <= 3.4028235e38f)) { f[i] = 0.f; bad = true; }
+}
+
+// The sequences' pieces are numbered so that no table is needed: sequence s has the numbers cu[s]/64 + 2 s and on, which are
+// at least as many as the blocks that its rows touch wherever they start (n/64 + 2).
+template <typename T, int D>
+__global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const StoreParams p) {
+  constexpr int kLanes = D / 8, kPass = kStoreThreads / kLanes, kIter = kBlockRows / kPass;
+  __shared__ float s_max[kStoreThreads / 32];
+  pdl_wait();
+  pdl_next();
+  const int tid = threadIdx.x, slot = blockIdx.x, head = blockIdx.y, side = blockIdx.z;
+  int below = 0;   // sequences whose first number is at most `slot`
+  for (int b0 = 0; b0 < p.c.batch; b0 += kStoreThreads) {
+    const int b = b0 + tid;
+    below += __syncthreads_count(b < p.c.batch && p.cu[min(b, p.c.batch - 1)] / kBlockRows + 2 * b <= slot);
+  }
+  const int b = below - 1;
+  if (b < 0) return;
+  const int c0 = p.cu[b], c1 = p.cu[b + 1], start = p.start ? p.start[b] : 0;
+  const int n = c1 - c0;
+  if (n == 0) return;
+  if (n < 0 || c0 < 0 || c1 > p.total || start < 0 || start > p.c.cap - n) {   // reported, nothing stored
+    if (tid == 0 && p.status) atomicOr(p.status, ST3_DEV_RANGE);
+    return;
+  }
+  const int blk = start / kBlockRows + (slot - (c0 / kBlockRows + 2 * b));
+  const int row0 = blk * kBlockRows;
+  if (row0 >= start + n) return;
+  const int lo = max(start - row0, 0), hi = min(start + n - row0, kBlockRows);   // new rows of this block
+  const size_t bh = (size_t)b * p.c.heads + head;
+  int8_t* codes = p.c.code[side] + (bh * p.c.cap + row0) * D;
+  float* scale = p.c.scale[side] + bh * (p.c.cap / kBlockRows) + blk;
+  const T* src = static_cast<const T*>(p.src[side]) + (long long)(c0 + row0 - start) * p.token_stride[side] +
+                 (long long)head * p.head_stride[side];
+  const int lane8 = (tid % kLanes) * 8, r0 = tid / kLanes;
+  float x[kIter][8];
+  float amax = 0.f;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < kIter; ++i) {
+    const int r = r0 + i * kPass;
+    if (r >= lo && r < hi) {
+      load8(src + (long long)r * p.token_stride[side] + lane8, x[i], bad);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[i][e]));
+    }
+  }
+  const float was = lo > 0 ? *scale : 0.f;   // read ahead of the barrier, written after it
+  amax = warp_max(amax);
+  if ((tid & 31) == 0) s_max[tid >> 5] = amax;
+  if (__syncthreads_or(bad) && tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
+#pragma unroll
+  for (int i = 0; i < kStoreThreads / 32; ++i) amax = fmaxf(amax, s_max[i]);
+  int e = block_exp(amax);
+  const int e_was = scale_exp(was);
+  if (lo > 0) e = max(e, e_was);
+  const float inv = exp2i(-e);
+#pragma unroll
+  for (int i = 0; i < kIter; ++i) {
+    const int r = r0 + i * kPass;
+    uint2* at = reinterpret_cast<uint2*>(codes + r * D + lane8);
+    if (r >= lo && r < hi) {
+      int c[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = code_of(x[i][j], inv);
+      *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+    } else if (r < lo && e > e_was) {
+      const uint2 w = *at;
+      const float f = exp2i(max(e_was - e, -126));
+      int c[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = code_of((float)byte_of(j < 4 ? w.x : w.y, j & 3), f);
+      *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+    }
+  }
+  if (tid == 0) *scale = exp2i(e);
+  if (side == 0 && tid >= lo && tid < hi) {
+    const size_t at = bh * p.c.cap + row0 + tid;
+    p.c.ids[at] = (p.pos ? p.pos[b] : start) + row0 + tid - start;
+    p.c.weights[at] = 0.f;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Rows out
+// ------------------------------------------------------------------------------------------------------------------
+struct RowsParams {
+  CacheView c;
+  void* dst[2];
+  int* ids;
+  float* weights;
+  const int* first;
+  const int* held;
+  int num_rows;
+};
+
+constexpr int kRowsThreads = 256;
+
+// A thread reads 16 codes and writes 16 values; K and V are two halves of the grid's last dimension.
+template <typename T, int D>
+__global__ void __launch_bounds__(kRowsThreads) st3_cache_rows_kernel(const RowsParams p) {
+  constexpr int kLanes = D / 16, kPer = kRowsThreads / kLanes;
+  pdl_wait();
+  pdl_next();
+  const int side = blockIdx.z & 1, h = blockIdx.y, b = blockIdx.z >> 1;
+  const int i = blockIdx.x * kPer + threadIdx.x / kLanes;
+  const int held = clamp_rows(p.held[b], p.c.cap);
+  const long long r = (long long)(p.first ? p.first[b] : 0) + i;
+  const bool live = r >= 0 && r < held;
+  const size_t bh = (size_t)b * p.c.heads + h;
+  // selected, not indexed: an index would put the parameters into local memory
+  T* dst = static_cast<T*>(side ? p.dst[1] : p.dst[0]);
+  const int8_t* codes = side ? p.c.code[1] : p.c.code[0];
+  const float* scales = side ? p.c.scale[1] : p.c.scale[0];
+  if (i < p.num_rows && dst) {
+    const int col = (threadIdx.x % kLanes) * 16;
+    uint4 w = make_uint4(0, 0, 0, 0);
+    float s = 0.f;
+    if (live) {
+      w = *reinterpret_cast<const uint4*>(codes + (bh * p.c.cap + r) * D + col);
+      s = scales[bh * (p.c.cap / kBlockRows) + r / kBlockRows];
+    }
+    const unsigned in[4] = {w.x, w.y, w.z, w.w};
+    float f[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) f[j] = (float)byte_of(in[j >> 2], j & 3) * s;
+    T* out = dst + (bh * p.num_rows + i) * D + col;
+    if constexpr (sizeof(T) == 2) {
+      unsigned o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const __nv_bfloat162 v2 = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+        o[j] = *reinterpret_cast<const unsigned*>(&v2);
+      }
+      reinterpret_cast<uint4*>(out)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      reinterpret_cast<uint4*>(out)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) reinterpret_cast<float4*>(out)[j] = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+    }
+  }
+  const int i2 = blockIdx.x * kPer + threadIdx.x;   // ids and weights: the first threads of the K half
+  if (side == 0 && threadIdx.x < kPer && i2 < p.num_rows) {
+    const long long r2 = (long long)(p.first ? p.first[b] : 0) + i2;
+    const bool live2 = r2 >= 0 && r2 < held;
+    if (p.ids) p.ids[bh * p.num_rows + i2] = live2 ? p.c.ids[bh * p.c.cap + r2] : 0;
+    if (p.weights) p.weights[bh * p.num_rows + i2] = live2 ? p.c.weights[bh * p.c.cap + r2] : 0.f;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Eviction: a thread block per (sequence, head) decides, then one per block of rows moves.
+// ------------------------------------------------------------------------------------------------------------------
+struct EvictParams {
+  CacheView from, to;
+  const int* held;
+  const int* seen;
+  int* held_out;
+  int* status;
+  int* src;            // [bh][cap_src] row that each row below the new length comes from
+  int* movers;         // [bh][cap]     kept rows from behind the new length, in order
+  int* changed;        // [bh][cap/64]  blocks that receive rows
+  int* length;         // [bh]          rows that stay
+  float* edge;         // [bh][2]       scales of the block that the new length cuts
+  int keep, recent, in_place;
+};
+
+constexpr int kEvictThreads = 1024;
+constexpr int kBins = 2048;
+
+// Weights as unsigned keys of the same order; -0 is 0, NaN the lowest, a recent row the highest.
+__device__ __forceinline__ unsigned weight_key(float w, bool recent) {
+  if (recent) return 0xffffffffu;
+  if (w != w) return 0u;
+  const unsigned b = __float_as_uint(w + 0.f);
+  return min((b & 0x80000000u) ? ~b : b | 0x80000000u, 0xfffffffeu);
+}
+
+__device__ __forceinline__ int block_sum_below(int x, int* s_warp, int& total) {   // exclusive sum over the block
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int v = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += y;
+  }
+  __syncthreads();
+  if (lane == 31) s_warp[warp] = v;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < kEvictThreads / 32; ++i) {
+    const int y = s_warp[i];
+    all += y;
+    if (i < warp) before += y;
+  }
+  total = all;
+  return before + v - x;
+}
+
+// The `want`-th element in descending order (1-based) of keys whose bits above `shift + bits` equal `prefix`: finds the bin
+// of the next `bits` bits and subtracts what lies above it.  All threads return the same.
+struct Pick { unsigned bin; int want; int in_bin; };
+
+__device__ __forceinline__ Pick pick_bin(const int* s_hist, int bins, int want, int* s_warp, int* s_out) {
+  // thread t sums the bins [t*per, ...) counted from the top
+  const int per = bins / kEvictThreads;
+  int mine = 0;
+  for (int j = 0; j < per; ++j) mine += s_hist[bins - 1 - (threadIdx.x * per + j)];
+  int total;
+  int above = block_sum_below(mine, s_warp, total);
+  if (above < want && want <= above + mine) {
+    for (int j = 0; j < per; ++j) {
+      const int bin = bins - 1 - (threadIdx.x * per + j), c = s_hist[bin];
+      if (want <= above + c) { s_out[0] = bin; s_out[1] = want - above; s_out[2] = c; break; }
+      above += c;
+    }
+  }
+  __syncthreads();
+  Pick r;
+  r.bin = (unsigned)s_out[0]; r.want = s_out[1]; r.in_bin = s_out[2];
+  __syncthreads();
+  return r;
+}
+
+__global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const EvictParams p) {
+  __shared__ int s_hist[kBins];
+  __shared__ int s_warp[kEvictThreads / 32];
+  __shared__ int s_out[3];
+  pdl_wait();
+  pdl_next();
+  const int tid = threadIdx.x, bh = blockIdx.x, b = bh / p.from.heads;
+  const int raw = p.held[b];
+  const int n = clamp_rows(raw, p.from.cap), k = min(n, p.keep);
+  const int blocks = p.from.cap / kBlockRows;
+  if (tid == 0) {
+    p.length[bh] = k;
+    if (raw != n && p.status) atomicOr(p.status, ST3_DEV_RANGE);
+    if (k < p.from.cap) {
+      p.edge[2 * bh] = p.from.scale[0][(size_t)bh * blocks + k / kBlockRows];
+      p.edge[2 * bh + 1] = p.from.scale[1][(size_t)bh * blocks + k / kBlockRows];
+    }
+  }
+  for (int i = tid; i < blocks; i += kEvictThreads) p.changed[(size_t)bh * blocks + i] = 0;
+  int* src = p.src + (size_t)bh * p.from.cap;
+  if (n <= p.keep) {
+    for (int i = tid; i < k; i += kEvictThreads) src[i] = i;
+    return;
+  }
+  const float* w = p.from.weights + (size_t)bh * p.from.cap;
+  const int* ids = p.from.ids + (size_t)bh * p.from.cap;
+  const int border = p.seen[b] - p.recent;   // the first position that counts as recent
+  // the key of the k-th row from the top, 11 + 11 + 10 bits at a time
+  unsigned prefix = 0;
+  int want = k, ties = 0;
+  bool nan = false;
+  const int shifts[3] = {21, 10, 0};
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = shifts[pass], bits = pass < 2 ? 11 : 10;
+    for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kEvictThreads) {
+      const float wi = w[i];
+      nan |= wi != wi;
+      const unsigned key = weight_key(wi, ids[i] >= border);
+      if (pass == 0 || (key >> (shift + bits)) == prefix) atomicAdd(&s_hist[(key >> shift) & ((1u << bits) - 1)], 1);
+    }
+    __syncthreads();
+    const Pick r = pick_bin(s_hist, pass < 2 ? 2048 : 1024, want, s_warp, s_out);
+    prefix = (prefix << bits) | r.bin;
+    want = r.want;
+    ties = r.in_bin;
+  }
+  const unsigned cut = prefix;   // rows above it stay, `want` of the `ties` rows at it do: those of the lowest positions
+  if (__syncthreads_or(nan) && tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
+  unsigned last = 0xffffffffu;   // the last position that stays at the cut
+  if (want < ties) {
+    unsigned pre = 0;
+    for (int pass = 0; pass < 3; ++pass) {   // the want-th smallest position = the want-th largest complement
+      const int shift = shifts[pass], bits = pass < 2 ? 11 : 10;
+      for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
+      __syncthreads();
+      for (int i = tid; i < n; i += kEvictThreads) {
+        const int id = ids[i];
+        if (weight_key(w[i], id >= border) == cut) {
+          const unsigned key = ~((unsigned)id ^ 0x80000000u);
+          if (pass == 0 || (key >> (shift + bits)) == pre) atomicAdd(&s_hist[(key >> shift) & ((1u << bits) - 1)], 1);
+        }
+      }
+      __syncthreads();
+      const Pick r = pick_bin(s_hist, pass < 2 ? 2048 : 1024, want, s_warp, s_out);
+      pre = (pre << bits) | r.bin;
+      want = r.want;
+    }
+    last = ~pre;
+  }
+  auto stays = [&](int i) {
+    const int id = ids[i];
+    const unsigned key = weight_key(w[i], id >= border);
+    return key > cut || (key == cut && ((unsigned)id ^ 0x80000000u) <= last);
+  };
+  // rows behind the new length that stay, in order
+  int* movers = p.movers + (size_t)bh * p.from.cap;
+  int base = 0;
+  for (int i0 = k; i0 < n; i0 += kEvictThreads) {
+    const int i = i0 + tid;
+    const int yes = i < n && stays(i);
+    int total;
+    const int at = base + block_sum_below(yes, s_warp, total);
+    if (yes) movers[at] = i;
+    base += total;
+  }
+  __syncthreads();
+  const int moved = base;
+  base = 0;
+  for (int i0 = 0; i0 < k; i0 += kEvictThreads) {
+    const int i = i0 + tid;
+    const int hole = i < k && !stays(i);
+    int total;
+    const int at = base + block_sum_below(hole, s_warp, total);
+    // positions that are not distinct could leave a hole without a mover; it then keeps its row
+    if (i < k) src[i] = hole && at < moved ? movers[at] : i;
+    if (hole) p.changed[(size_t)bh * blocks + i / kBlockRows] = 1;
+    base += total;
+  }
+}
+
+constexpr int kMoveThreads = 256;
+
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads) st3_cache_move_kernel(const EvictParams p) {
+  constexpr int kLanes = D / 16, kIter = kBlockRows * kLanes / kMoveThreads;   // 16-byte pieces of a row; pieces a thread
+  static_assert(kBlockRows * (64 / 16) % kMoveThreads == 0, "pieces");
+  __shared__ int s_src[kBlockRows];
+  __shared__ float s_scale[2][kBlockRows];
+  __shared__ float s_max[2][kMoveThreads / 32];
+  pdl_wait();
+  pdl_next();
+  const int tid = threadIdx.x, bh = blockIdx.y, blk = blockIdx.x;
+  const int k = p.length[bh], row0 = blk * kBlockRows;
+  if (blk == 0 && bh % p.from.heads == 0 && tid == 0) p.held_out[bh / p.from.heads] = k;
+  if (row0 >= k) return;
+  const int from_blocks = p.from.cap / kBlockRows;
+  const bool changed = p.changed[(size_t)bh * from_blocks + blk];
+  if (p.in_place && !changed) return;
+  const int rows = min(k - row0, kBlockRows);
+  if (tid < kBlockRows) {
+    const int s = tid < rows ? p.src[(size_t)bh * p.from.cap + row0 + tid] : 0;
+    s_src[tid] = s;
+    // in place the scale of the block that the new length cuts may already be that of the rows moved into it
+    const bool edge = s >= k && s / kBlockRows == k / kBlockRows;
+#pragma unroll
+    for (int side = 0; side < 2; ++side)
+      s_scale[side][tid] = edge ? p.edge[2 * bh + side] : p.from.scale[side][(size_t)bh * from_blocks + s / kBlockRows];
+  }
+  __syncthreads();
+  uint4 piece[2][kIter];
+  float amax[2] = {0.f, 0.f};
+#pragma unroll
+  for (int side = 0; side < 2; ++side)
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      const int at = tid + i * kMoveThreads, r = at / kLanes, col = (at % kLanes) * 16;
+      if (r < rows) piece[side][i] = *reinterpret_cast<const uint4*>(p.from.code[side] + ((size_t)bh * p.from.cap + s_src[r]) * D + col);
+    }
+#pragma unroll
+  for (int side = 0; side < 2; ++side)
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      const int r = (tid + i * kMoveThreads) / kLanes;
+      if (r < rows) {
+        const unsigned w[4] = {piece[side][i].x, piece[side][i].y, piece[side][i].z, piece[side][i].w};
+        int m = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) m = max(m, abs(byte_of(w[j >> 2], j & 3)));
+        amax[side] = fmaxf(amax[side], (float)m * s_scale[side][r]);
+      }
+    }
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const float m = warp_max(amax[side]);
+    if ((tid & 31) == 0) s_max[side][tid >> 5] = m;
+  }
+  __syncthreads();   // every row of this block has been read, too
+  const int to_blocks = p.to.cap / kBlockRows;
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMoveThreads / 32; ++i) m = fmaxf(m, s_max[side][i]);
+    // a block without a hole keeps its scale
+    const int e = changed ? block_exp(m) : scale_exp(s_scale[side][0]);
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      const int at = tid + i * kMoveThreads, r = at / kLanes, col = (at % kLanes) * 16;
+      if (r < rows) {
+        const int d = scale_exp(s_scale[side][r]) - e;
+        uint4 o = piece[side][i];
+        if (d) {
+          const float f = exp2i(max(d, -126));
+          unsigned w[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            w[j] = pack4(code_of((float)byte_of(w[j], 0), f), code_of((float)byte_of(w[j], 1), f),
+                         code_of((float)byte_of(w[j], 2), f), code_of((float)byte_of(w[j], 3), f));
+          o = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        *reinterpret_cast<uint4*>(p.to.code[side] + ((size_t)bh * p.to.cap + row0 + r) * D + col) = o;
+      }
+    }
+    if (tid == 0) p.to.scale[side][(size_t)bh * to_blocks + blk] = exp2i(e);
+  }
+  if (tid < rows) {
+    const size_t from = (size_t)bh * p.from.cap + s_src[tid], to = (size_t)bh * p.to.cap + row0 + tid;
+    p.to.ids[to] = p.from.ids[from];
+    p.to.weights[to] = p.from.weights[from];
+  }
+}
+
+}  // namespace
+
+#include "st3_cache_attend.cuh"
+
+// ------------------------------------------------------------------------------------------------------------------
+// C ABI
+// ------------------------------------------------------------------------------------------------------------------
+namespace {
+
+bool aligned16(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+st3_status check_shape(const st3_cache* c) {
+  if (!c) return ST3_ERR_INVALID_ARG;
+  if (c->batch < 1 || c->num_kv_heads < 1 || c->capacity < 1 || c->capacity % kBlockRows) return ST3_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return ST3_ERR_UNSUPPORTED;
+  // rows are numbered with 31 bits (codes of up to 2^38 bytes); the grids' second and third dimensions
+  if ((long long)c->batch * c->num_kv_heads * c->capacity > 0x7fffffffLL) return ST3_ERR_UNSUPPORTED;
+  if (c->batch > 32767 || c->num_kv_heads > 65535 || (long long)c->batch * c->num_kv_heads > 65535) return ST3_ERR_UNSUPPORTED;
+  return ST3_OK;
+}
+st3_status check_cache(const st3_cache* c) {
+  const st3_status st = check_shape(c);
+  if (st != ST3_OK) return st;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_scale) || !aligned16(c->v_scale) || !aligned16(c->ids) || !aligned16(c->weights))
+    return ST3_ERR_INVALID_ARG;
+  return ST3_OK;
+}
+CacheView view_of(const st3_cache* c) {
+  CacheView v;
+  v.code[0] = c->k; v.code[1] = c->v;
+  v.scale[0] = c->k_scale; v.scale[1] = c->v_scale;
+  v.ids = c->ids; v.weights = c->weights;
+  v.batch = c->batch; v.heads = c->num_kv_heads; v.cap = c->capacity;
+  return v;
+}
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+extern "C" st3_status st3_cache_store(const st3_cache* cache, const void* k, const void* v, int32_t dtype,
+                                      int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                                      int64_t v_head_stride, const int32_t* cu, int32_t total, const int32_t* start,
+                                      const int32_t* pos, int* dev_status, void* cuda_stream) {
+  const st3_status st = check_cache(cache);
+  if (st != ST3_OK) return st;
+  if (total < 0 || !aligned4(cu) || (start && !aligned4(start)) || (pos && !aligned4(pos))) return ST3_ERR_INVALID_ARG;
+  if (dtype != ST3_BF16 && dtype != ST3_F32) return ST3_ERR_UNSUPPORTED;
+  if (total == 0) return ST3_OK;
+  if (!aligned16(k) || !aligned16(v)) return ST3_ERR_INVALID_ARG;
+  const int unit = dtype == ST3_BF16 ? 8 : 4;   // elements of 16 bytes
+  for (int64_t s : {k_token_stride, k_head_stride, v_token_stride, v_head_stride})
+    if (s < 0 || s % unit) return ST3_ERR_INVALID_ARG;
+  StoreParams p;
+  p.c = view_of(cache);
+  p.src[0] = k; p.src[1] = v;
+  p.token_stride[0] = k_token_stride; p.token_stride[1] = v_token_stride;
+  p.head_stride[0] = k_head_stride; p.head_stride[1] = v_head_stride;
+  p.cu = cu; p.start = start; p.pos = pos; p.status = dev_status; p.total = total;
+  const dim3 grid((unsigned)(total / kBlockRows + 2 * cache->batch), (unsigned)cache->num_kv_heads, 2);
+  const dim3 block(kStoreThreads);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (dtype == ST3_BF16)
+    return cache->head_dim == 128 ? launch(st3_cache_store_kernel<__nv_bfloat16, 128>, grid, block, 0, s, p)
+                                  : launch(st3_cache_store_kernel<__nv_bfloat16, 64>, grid, block, 0, s, p);
+  return cache->head_dim == 128 ? launch(st3_cache_store_kernel<float, 128>, grid, block, 0, s, p)
+                                : launch(st3_cache_store_kernel<float, 64>, grid, block, 0, s, p);
+}
+
+extern "C" st3_status st3_cache_rows(const st3_cache* cache, const int32_t* first, const int32_t* held,
+                                     int32_t num_rows, void* k, void* v, int32_t dtype, int32_t* ids, float* weights,
+                                     void* cuda_stream) {
+  const st3_status st = check_cache(cache);
+  if (st != ST3_OK) return st;
+  if (num_rows < 0 || !aligned4(held) || (first && !aligned4(first)) || (k && !aligned16(k)) || (v && !aligned16(v)) ||
+      (ids && !aligned4(ids)) || (weights && !aligned4(weights)))
+    return ST3_ERR_INVALID_ARG;
+  if (dtype != ST3_BF16 && dtype != ST3_F32) return ST3_ERR_UNSUPPORTED;
+  if (num_rows == 0) return ST3_OK;
+  RowsParams p;
+  p.c = view_of(cache);
+  p.dst[0] = k; p.dst[1] = v; p.ids = ids; p.weights = weights; p.first = first; p.held = held; p.num_rows = num_rows;
+  const int per = kRowsThreads / (cache->head_dim / 16);
+  const dim3 grid((unsigned)((num_rows + per - 1) / per), (unsigned)cache->num_kv_heads, 2 * (unsigned)cache->batch);
+  const dim3 block(kRowsThreads);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (dtype == ST3_BF16)
+    return cache->head_dim == 128 ? launch(st3_cache_rows_kernel<__nv_bfloat16, 128>, grid, block, 0, s, p)
+                                  : launch(st3_cache_rows_kernel<__nv_bfloat16, 64>, grid, block, 0, s, p);
+  return cache->head_dim == 128 ? launch(st3_cache_rows_kernel<float, 128>, grid, block, 0, s, p)
+                                : launch(st3_cache_rows_kernel<float, 64>, grid, block, 0, s, p);
+}
+
+namespace {
+struct EvictLayout { size_t src, movers, changed, length, edge, total; };
+EvictLayout evict_layout(const st3_cache* c) {
+  const size_t bh = (size_t)c->batch * c->num_kv_heads;
+  EvictLayout l;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t x = at; at += up256(bytes); return x; };
+  l.src = take(bh * c->capacity * 4);
+  l.movers = take(bh * c->capacity * 4);
+  l.changed = take(bh * (c->capacity / kBlockRows) * 4);
+  l.length = take(bh * 4);
+  l.edge = take(bh * 8);
+  l.total = at;
+  return l;
+}
+}  // namespace
+
+extern "C" st3_status st3_cache_evict_workspace(const st3_cache* from, size_t* bytes) {
+  const st3_status st = check_shape(from);
+  if (st != ST3_OK) return st;
+  if (!bytes) return ST3_ERR_INVALID_ARG;
+  *bytes = evict_layout(from).total;
+  return ST3_OK;
+}
+
+extern "C" st3_status st3_cache_evict(const st3_cache* from, const st3_cache* to, const int32_t* held,
+                                      const int32_t* seen, int32_t keep, int32_t recent, int32_t* held_out,
+                                      void* workspace, size_t bytes, int* dev_status, void* cuda_stream) {
+  st3_status st = check_cache(from);
+  if (st == ST3_OK) st = check_cache(to);
+  if (st != ST3_OK) return st;
+  if (from->batch != to->batch || from->num_kv_heads != to->num_kv_heads || from->head_dim != to->head_dim) return ST3_ERR_INVALID_ARG;
+  if (keep < 1 || recent < 0 || recent > keep || !aligned4(held) || !aligned4(seen) || !aligned4(held_out)) return ST3_ERR_INVALID_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ST3_ERR_INVALID_ARG;
+  // in place is all arrays in place
+  const int same = (from->k == to->k) + (from->v == to->v) + (from->k_scale == to->k_scale) + (from->v_scale == to->v_scale) +
+                   (from->ids == to->ids) + (from->weights == to->weights);
+  if (same != 0 && (same != 6 || from->capacity != to->capacity)) return ST3_ERR_INVALID_ARG;
+  if (to->capacity < keep && to->capacity < from->capacity) return ST3_ERR_CAPACITY;
+  const EvictLayout l = evict_layout(from);
+  if (bytes < l.total) return ST3_ERR_WORKSPACE_TOO_SMALL;
+  char* ws = static_cast<char*>(workspace);
+  EvictParams p;
+  p.from = view_of(from); p.to = view_of(to);
+  p.held = held; p.seen = seen; p.held_out = held_out; p.status = dev_status;
+  p.src = reinterpret_cast<int*>(ws + l.src);
+  p.movers = reinterpret_cast<int*>(ws + l.movers);
+  p.changed = reinterpret_cast<int*>(ws + l.changed);
+  p.length = reinterpret_cast<int*>(ws + l.length);
+  p.edge = reinterpret_cast<float*>(ws + l.edge);
+  p.keep = keep; p.recent = recent; p.in_place = same == 6;
+  const unsigned bh = (unsigned)(from->batch * from->num_kv_heads);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  st = launch(st3_cache_select_kernel, dim3(bh), dim3(kEvictThreads), 0, s, p);
+  if (st != ST3_OK) return st;
+  const int most = keep < from->capacity ? keep : from->capacity;
+  const dim3 grid((unsigned)((most + kBlockRows - 1) / kBlockRows), bh);
+  return from->head_dim == 128 ? launch(st3_cache_move_kernel<128>, grid, dim3(kMoveThreads), 0, s, p)
+                               : launch(st3_cache_move_kernel<64>, grid, dim3(kMoveThreads), 0, s, p);
+}
+
+namespace {
+
+struct AttendLayout { size_t ml, acc, logits, total; int group, passes, pitch, grid; };
+AttendLayout attend_layout(const st3_cache* c, int heads, bool weights) {
+  AttendLayout l;
+  l.group = heads / c->num_kv_heads;
+  l.passes = (l.group + kCaHeads - 1) / kCaHeads;
+  l.pitch = l.group <= 8 ? 8 : kCaHeads;
+  const long long blocks = (long long)c->batch * c->num_kv_heads * l.passes * (c->capacity / kBlockRows);
+  l.grid = blocks < kCaGrid ? (int)blocks : kCaGrid;
+  const size_t slots = (size_t)l.grid + (size_t)c->batch * c->num_kv_heads * l.passes;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t x = at; at += up256(bytes); return x; };
+  l.ml = take(slots * l.pitch * 3 * 4);
+  l.acc = take(slots * l.pitch * c->head_dim * 4);
+  l.logits = take(weights ? (size_t)c->batch * heads * c->capacity * 4 : 0);
+  l.total = at;
+  return l;
+}
+
+bool make_code_map(EncodeTiledFn fn, CUtensorMap* map, const st3_cache* c, const int8_t* base) {
+  const cuuint64_t rows = (cuuint64_t)c->batch * c->num_kv_heads * c->capacity;
+  const cuuint64_t dims[2] = {(cuuint64_t)c->head_dim, rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)c->head_dim};
+  const cuuint32_t box[2] = {(cuuint32_t)c->head_dim, kBlockRows};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            c->head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int D, int kTiles>
+st3_status attend_launch(const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttendParams& p, cudaStream_t s) {
+  if (cudaFuncSetAttribute(st3_cache_attend_kernel<T, D, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, CaLayout<D>::kTotal) != cudaSuccess)
+    return ST3_ERR_CUDA;
+  st3_status st = launch(st3_cache_attend_kernel<T, D, kTiles>, dim3((unsigned)p.grid), dim3(kCaThreads), CaLayout<D>::kTotal, s, mk, mv, p);
+  if (st != ST3_OK) return st;
+  const unsigned chunks = p.weights_out ? (unsigned)((p.c.cap + kCaChunk - 1) / kCaChunk) : 0u;
+  return launch(st3_cache_merge_kernel<T, D>, dim3((unsigned)(p.c.batch * p.c.heads), (unsigned)p.passes + chunks), dim3(kCaMergeThreads), 0, s, p);
+}
+
+st3_status check_heads(const st3_cache* c, int heads) {
+  if (heads < 1 || heads % c->num_kv_heads) return ST3_ERR_INVALID_ARG;
+  if (heads / c->num_kv_heads > 1024 || (long long)c->batch * heads * c->capacity > 0x7fffffffffLL) return ST3_ERR_UNSUPPORTED;
+  const long long passes = (heads / c->num_kv_heads + kCaHeads - 1) / kCaHeads;
+  if ((long long)c->batch * c->num_kv_heads * passes * (c->capacity / kBlockRows) > 0x3fffffffLL) return ST3_ERR_UNSUPPORTED;
+  if (passes + c->capacity / kCaChunk + 1 > 65535) return ST3_ERR_UNSUPPORTED;
+  return ST3_OK;
+}
+
+}  // namespace
+
+extern "C" st3_status st3_cache_attend_workspace(const st3_cache* cache, int32_t num_heads, int32_t with_weights, size_t* bytes) {
+  st3_status st = check_shape(cache);
+  if (st == ST3_OK) st = check_heads(cache, num_heads);
+  if (st != ST3_OK) return st;
+  if (!bytes) return ST3_ERR_INVALID_ARG;
+  *bytes = attend_layout(cache, num_heads, with_weights != 0).total;
+  return ST3_OK;
+}
+
+extern "C" st3_status st3_cache_attend(const st3_cache* cache, const void* q, void* out, int32_t dtype, int32_t num_heads,
+                                       const int32_t* held, const float* weights_in, float* weights_out,
+                                       void* workspace, size_t bytes, int* dev_status, void* cuda_stream) {
+  st3_status st = check_cache(cache);
+  if (st == ST3_OK) st = check_heads(cache, num_heads);
+  if (st != ST3_OK) return st;
+  if (!aligned16(q) || !aligned16(out) || !aligned4(held) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ST3_ERR_INVALID_ARG;
+  if (weights_out && (!aligned4(weights_in) || !aligned4(weights_out))) return ST3_ERR_INVALID_ARG;
+  if (dtype != ST3_BF16 && dtype != ST3_F32) return ST3_ERR_UNSUPPORTED;
+  const AttendLayout l = attend_layout(cache, num_heads, weights_out != nullptr);
+  if (bytes < l.total) return ST3_ERR_WORKSPACE_TOO_SMALL;
+  const EncodeTiledFn encode = tensor_map_encoder();
+  CUtensorMap mk, mv;
+  if (!encode || !make_code_map(encode, &mk, cache, cache->k) || !make_code_map(encode, &mv, cache, cache->v)) return ST3_ERR_CUDA;
+  char* ws = static_cast<char*>(workspace);
+  CacheAttendParams p;
+  p.c = view_of(cache);
+  p.q = q; p.out = out; p.held = held; p.weights_in = weights_in; p.weights_out = weights_out; p.status = dev_status;
+  p.part_ml = reinterpret_cast<float*>(ws + l.ml);
+  p.part_acc = reinterpret_cast<float*>(ws + l.acc);
+  p.logits = weights_out ? reinterpret_cast<float*>(ws + l.logits) : nullptr;
+  p.group = l.group; p.passes = l.passes; p.pitch = l.pitch; p.grid = l.grid;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const bool wide = l.group > 8, d128 = cache->head_dim == 128;
+  if (dtype == ST3_BF16) {
+    if (d128) return wide ? attend_launch<__nv_bfloat16, 128, 2>(mk, mv, p, s) : attend_launch<__nv_bfloat16, 128, 1>(mk, mv, p, s);
+    return wide ? attend_launch<__nv_bfloat16, 64, 2>(mk, mv, p, s) : attend_launch<__nv_bfloat16, 64, 1>(mk, mv, p, s);
+  }
+  if (d128) return wide ? attend_launch<float, 128, 2>(mk, mv, p, s) : attend_launch<float, 128, 1>(mk, mv, p, s);
+  return wide ? attend_launch<float, 64, 2>(mk, mv, p, s) : attend_launch<float, 64, 1>(mk, mv, p, s);
+}

@@ -1,0 +1,632 @@
+// One query per head over the 8-bit cache; included by st3_cache.cu only.
+//
+// What bounds it: the codes, 2 D bytes a row and key/value head, read once for all query heads of the group.  At one byte an
+// element a group of four does 8 flops a byte, beyond what the fp32 pipes keep up with, so the products run on mma.sync
+// (m16n8k16, f16 x f16 -> fp32): codes are exact in f16, the query is scaled by a power of two into f16's range (bf16 fits
+// exactly, fp32 is split in two halves of 11 bits), and the accumulators are fp32.  tcgen05 has nothing to win here: its
+// 128 rows of M would hold 1 to 16 queries.
+//
+// Work: the blocks of 64 rows of all (sequence, head) pairs, end to end, cut into equal runs, one for each thread block of
+// one wave (two to an SM), so that ragged lengths and single long sequences fill the GPU alike.  What a run holds of one pair
+// is a segment; a segment leaves one partial (max, sum, un-normalised output), and a second launch joins the partials and
+// adds the probabilities to the accumulated weights from the logits left by the first.  Thread block c and pair i share at
+// most one segment, and along the runs either c or i grows from one segment to the next: c + i numbers them without a table.
+//
+// A producer warp brings whole blocks by TMA (K and V, 8 KB each at D = 128) into a ring; four consumer warps take 16 rows
+// of a block each.  The codes lie in shared memory as TMA's swizzle puts them, so that ldmatrix reads without bank conflicts:
+// for S = K q^T a register holds four neighbouring dims of a row, which become two f16 pairs; for O^T = V^T P^T ldmatrix
+// transposes 16-bit units, and a register holds two neighbouring dims of two rows, which become two pairs of rows.
+#ifndef ST3_CACHE_ATTEND_CUH_
+#define ST3_CACHE_ATTEND_CUH_
+
+namespace {
+
+constexpr int kCaGrid = 2 * 148;       // one wave
+constexpr int kCaConsumers = 4;
+constexpr int kCaThreads = (kCaConsumers + 1) * 32;
+constexpr int kCaHeads = 16;           // query heads of one pass over a group's rows; larger groups take several
+constexpr int kCaChunk = 1024;         // rows of the second launch's blocks that add weights
+constexpr int kCaMergeThreads = 256;
+
+struct CacheAttendParams {
+  CacheView c;
+  const void* q;
+  void* out;
+  const int* held;
+  const float* weights_in;
+  float* weights_out;
+  int* status;
+  float* part_ml;    // [segment][heads of a pass][3]: max of the logits, max of logit + log2(V scale), sum
+  float* part_acc;   // [segment][heads of a pass][D]
+  float* logits;     // [(sequence, kv head)][row][group] in the log2 domain, or null
+  int group;         // query heads per key/value head
+  int passes;        // ceil(group / kCaHeads)
+  int pitch;         // heads of a pass, rounded up to 8
+  int grid;
+};
+
+template <int D>
+struct CaLayout {
+  static constexpr int kSide = kBlockRows * D;               // bytes of a block's K or V
+  static constexpr int kStage = 2 * kSide;
+  static constexpr int kStages = 80 * 1024 / kStage;
+  static constexpr int kPitch = D + 4;                       // floats from one head's sums to the next: no bank conflicts
+  static constexpr int kRed = kStages * kStage;              // sums of the four warps, 8 heads at a time
+  static constexpr int kBars = kRed + kCaConsumers * 8 * kPitch * 4;
+  static constexpr int kMl = kBars + 2 * kStages * 8;
+  static constexpr int kTotal = kMl + kCaConsumers * kCaHeads * 3 * 4 + 64;
+};
+
+// The run of thread block c: blocks [total * c / grid, total * (c + 1) / grid), with grid <= total, so that none is empty.
+__device__ __forceinline__ int run_start(int total, int c, int grid) { return (int)((long long)total * c / grid); }
+// The thread block whose run holds block x.
+__device__ __forceinline__ int run_of(int total, int x, int grid) { return (int)((((long long)x + 1) * grid - 1) / total); }
+__device__ __forceinline__ int blocks_of(const CacheAttendParams& p, int b) {
+  return (clamp_rows(p.held[b], p.c.cap) + kBlockRows - 1) / kBlockRows;
+}
+
+__device__ __forceinline__ void tma_rows(void* dst, const CUtensorMap* map, int row, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
+      "l"(map), "r"(0), "r"(row), "r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ bool ca_wait(uint64_t* bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > kWaitCycles) return false;
+  return true;
+}
+__device__ __forceinline__ void ca_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// A barrier of the consumer warps that tells each of them whether any has failed.
+__device__ __forceinline__ bool ca_any_failed(bool failed) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, 1, %2, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)failed), "n"(kCaConsumers * 32)
+      : "memory");
+  return any != 0;
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// Two codes of a word as f16: biased by 128 they are the low bits of 1024 + u, from which 1152 is taken.  `flipped` is the
+// word with every code's sign bit inverted.
+template <int kSel>
+__device__ __forceinline__ uint32_t codes_f16(uint32_t flipped) {
+  const uint32_t w = __byte_perm(flipped, 0x64646464u, kSel);
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// what rounding the pair to f16 has lost, as another pair
+__device__ __forceinline__ uint32_t half_rest(float a, float b, uint32_t hi) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  return half_pair(a - f.x, b - f.y);
+}
+
+// kTiles: groups of 8 query heads of a pass.  fp32 queries and probabilities go in as two f16 terms each.
+template <typename T, int D, int kTiles>
+__global__ void __launch_bounds__(kCaThreads, 2)
+st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheAttendParams p) {
+  using L = CaLayout<D>;
+  constexpr int kTerms = sizeof(T) == 4 ? 2 : 1;
+  constexpr int kSteps = D / 16;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
+  uint64_t* empty = full + L::kStages;
+  float* s_ml = reinterpret_cast<float*>(smem + L::kMl);
+  int* s_int = reinterpret_cast<int*>(s_ml + kCaConsumers * kCaHeads * 3);   // 16 ints
+  float* s_red = reinterpret_cast<float*>(smem + L::kRed);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < L::kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], kCaConsumers); }
+    mbar_fence_init();
+    s_int[8] = 0;
+  }
+  if (smem_u32(smem) & 1023u) {   // the swizzle assumes aligned tiles: reported, nothing computed
+    if (tid == 0 && p.status) atomicOr(p.status, ST3_DEV_RANGE);
+    pdl_wait();
+    return;
+  }
+  pdl_wait();
+  pdl_next();
+  // ---- this block's run, and the sequence that its first block lies in ----
+  const int per = (p.c.batch + kCaThreads - 1) / kCaThreads, pairs = p.c.heads * p.passes;
+  int mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int b = tid * per + i;
+    if (b < p.c.batch) {
+      mine += blocks_of(p, b);
+      if (blockIdx.x == 0 && p.status && p.held[b] != clamp_rows(p.held[b], p.c.cap)) atomicOr(p.status, ST3_DEV_RANGE);
+    }
+  }
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  if (lane == 31) s_int[warp] = incl;
+  __syncthreads();
+  int before = incl - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w <= kCaConsumers; ++w) {
+    if (w < warp) before += s_int[w];
+    total += s_int[w];
+  }
+  total *= pairs;
+  before *= pairs;   // blocks of all pairs in front of this thread's first sequence
+  const int grid = min(p.grid, total);
+  const bool works = (int)blockIdx.x < grid;
+  const int x0 = works ? run_start(total, blockIdx.x, grid) : 0, x1 = works ? run_start(total, blockIdx.x + 1, grid) : 0;
+  if (x0 < x1 && x0 >= before && x0 < before + mine * pairs) {
+    int b = tid * per;
+    for (;; ++b) {
+      const int nb = blocks_of(p, b) * pairs;
+      if (x0 < before + nb) break;
+      before += nb;
+    }
+    s_int[6] = b;
+    s_int[7] = before;
+  }
+  __syncthreads();
+  if (x0 >= x1) return;
+  int b = s_int[6], x = x0, seq0 = s_int[7];
+  volatile int* fail = s_int + 8;
+
+  if (warp == kCaConsumers) {
+    // ===================== producer =====================
+    if (lane == 0) {
+      bool ok = true;
+      int stage = 0, parity = 1, issued = 0;
+      while (x < x1 && ok) {
+        int nb = blocks_of(p, b);
+        while (x >= seq0 + nb * pairs) { seq0 += nb * pairs; nb = blocks_of(p, ++b); }
+        const int pair = (x - seq0) / nb, head = pair / p.passes;
+        const int i0 = x - seq0 - pair * nb, i1 = min(nb, i0 + x1 - x);
+        const int row = (b * p.c.heads + head) * p.c.cap;
+        for (int i = i0; i < i1; ++i) {
+          if (!ca_wait(&empty[stage], parity) || *fail) { ok = false; break; }
+          unsigned char* dst = smem + stage * L::kStage;
+          mbar_expect_tx(&full[stage], L::kStage);
+          tma_rows(dst, &map_k, row + i * kBlockRows, &full[stage]);
+          tma_rows(dst + L::kSide, &map_v, row + i * kBlockRows, &full[stage]);
+          ++issued;
+          if (++stage == L::kStages) { stage = 0; parity ^= 1; }
+        }
+        x += i1 - i0;
+      }
+      if (!ok) {
+        *fail = 1;
+        if (p.status) atomicOr(p.status, ST3_DEV_COPY_TIMEOUT);
+      }
+      // shared memory is not given back before the copies into it have landed, also where a consumer gave up
+      for (int u = max(0, issued - L::kStages); u < issued; ++u) ca_wait(&full[u % L::kStages], (u / L::kStages) & 1);
+    }
+    return;
+  }
+
+  // ===================== consumers =====================
+  const int g = lane >> 2, t = lane & 3;
+  const float sc = 1.4426950408889634f * rsqrtf((float)D);
+  const uint32_t ring = smem_u32(smem);
+  // ldmatrix addresses inside a block: row 16 warp + (lane & 15) for K and V; the lane's 16-byte chunk is 2 i + (lane >> 4)
+  const int lrow = warp * 16 + (lane & 15);
+  const int lxor = D == 128 ? (lrow & 7) : ((lrow >> 1) & 3);
+  const uint32_t lbase = (uint32_t)(lrow * D);
+  int stage = 0;
+  uint32_t parity = 0;
+  bool ok = true;
+  while (x < x1) {
+    int nb = blocks_of(p, b);
+    while (x >= seq0 + nb * pairs) { seq0 += nb * pairs; nb = blocks_of(p, ++b); }
+    const int pair = (x - seq0) / nb, head = pair / p.passes, h0 = (pair - head * p.passes) * kCaHeads;
+    const int heads = min(p.group - h0, kCaHeads);   // of this pass
+    const int i0 = x - seq0 - pair * nb, i1 = min(nb, i0 + x1 - x);
+    const int held = clamp_rows(p.held[b], p.c.cap);
+    const size_t bh = (size_t)b * p.c.heads + head;
+    const float* ks = p.c.scale[0] + bh * (p.c.cap / kBlockRows);
+    const float* vs = p.c.scale[1] + bh * (p.c.cap / kBlockRows);
+    // ---- the queries of this pass as B fragments: lane (g, t) holds head g, dims 16 i + 4 t .. + 3 ----
+    uint32_t qf[kTerms][kTiles][kSteps][2];
+    float qs[kTiles][2];   // factor of the logits of heads 2 t and 2 t + 1
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      const int hq = n * 8 + g;
+      float f[kSteps][4];
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        f[i][0] = f[i][1] = f[i][2] = f[i][3] = 0.f;
+        if (hq < heads) {
+          const T* src = static_cast<const T*>(p.q) + (((size_t)b * p.c.heads + head) * p.group + h0 + hq) * D + 16 * i + 4 * t;
+          if constexpr (sizeof(T) == 2) {
+            const uint2 w = *reinterpret_cast<const uint2*>(src);
+            f[i][0] = __uint_as_float(w.x << 16); f[i][1] = __uint_as_float(w.x & 0xffff0000u);
+            f[i][2] = __uint_as_float(w.y << 16); f[i][3] = __uint_as_float(w.y & 0xffff0000u);
+          } else {
+            const float4 w = *reinterpret_cast<const float4*>(src);
+            f[i][0] = w.x; f[i][1] = w.y; f[i][2] = w.z; f[i][3] = w.w;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(f[i][e]));
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // |q| * 2^-e lies in [2^13, 2^14): f16 keeps its 11 bits down to 2^-27 of the largest element
+      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 13, -100), 114);
+      const float down = exp2i(-e), up = exp2i(e);
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const float a = f[i][2 * w] * down, c = f[i][2 * w + 1] * down;
+          qf[0][n][i][w] = half_pair(a, c);
+          if constexpr (kTerms == 2) qf[kTerms - 1][n][i][w] = half_rest(a, c, qf[0][n][i][w]);
+        }
+      }
+      qs[n][0] = sc * __shfl_sync(0xffffffffu, up, 8 * t);
+      qs[n][1] = sc * __shfl_sync(0xffffffffu, up, 8 * t + 4);
+    }
+    // m: running maximum of a head's logits, l: sum of exp2(s - m) over this lane's rows; mv: running maximum of
+    // s + log2(V scale), which the probabilities that meet V are relative to, so that blocks of any scale share one
+    // accumulator and the largest term is 1.
+    float m[kTiles][2], mv[kTiles][2], l[kTiles][2];
+    float acc[kTiles][kSteps][4];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      m[n][0] = m[n][1] = mv[n][0] = mv[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
+    }
+    float ks32 = 0.f, vs32 = 0.f;   // the scales of 32 blocks, one a lane
+    for (int i = i0; i < i1; ++i) {
+      const int at = (i - i0) & 31;
+      if (at == 0) {
+        const int j = min(i + lane, i1 - 1);
+        ks32 = ks[j];
+        vs32 = vs[j];
+      }
+      const float kscale = exp2i(scale_exp(__shfl_sync(0xffffffffu, ks32, at)));
+      const float vexp = (float)scale_exp(__shfl_sync(0xffffffffu, vs32, at));
+      if (ok) ok = __all_sync(0xffffffffu, ca_wait(&full[stage], parity)) && !*fail;
+      if (!ok) break;
+      const uint32_t kb = ring + stage * L::kStage + lbase, vb = kb + L::kSide;
+      // ---- S = K q^T: 16 rows x 8 heads a tile ----
+      float s[kTiles][4];
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+      float s2[kTiles][4];   // every other step, a second chain
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) s2[n][0] = s2[n][1] = s2[n][2] = s2[n][3] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kSteps; c += 2) {
+        uint32_t r[4];
+        ldsm4(r, kb + (((c + (lane >> 4)) ^ lxor) << 4));
+        // matrices: rows 0-7 and 8-15 of chunk c, then of chunk c + 1
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] ^= 0x80808080u;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t a0 = codes_f16<0x4140>(r[2 * j]), a1 = codes_f16<0x4140>(r[2 * j + 1]);
+          const uint32_t a2 = codes_f16<0x4342>(r[2 * j]), a3 = codes_f16<0x4342>(r[2 * j + 1]);
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int term = 0; term < kTerms; ++term)
+              mma_f16(j ? s2[n] : s[n], a0, a1, a2, a3, qf[term][n][c + j][0], qf[term][n][c + j][1]);
+        }
+      }
+      // ---- softmax over this warp's 16 rows; lane: rows g and g + 8, heads 2 t and 2 t + 1 ----
+      const int row = i * kBlockRows + warp * 16 + g;
+      const bool in0 = row < held, in1 = row + 8 < held;
+      uint32_t pf[kTerms][kTiles][2];
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = ((e < 2) ? in0 : in1) ? (s[n][e] + s2[n][e]) * (kscale * qs[n][e & 1]) : -INFINITY;
+        if (p.logits) {
+          float* dst = p.logits + ((size_t)bh * p.c.cap + row) * p.group + h0 + n * 8 + 2 * t;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (((e < 2) ? in0 : in1) && n * 8 + 2 * t + (e & 1) < heads) dst[(e >> 1) * 8 * p.group + (e & 1)] = v[e];
+        }
+        float top[2] = {fmaxf(v[0], v[2]), fmaxf(v[1], v[3])};
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], o));
+          top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], o));
+        }
+        float ref[2], refv[2];
+        bool grown = false;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float m1 = fmaxf(m[n][j], top[j]), mv1 = fmaxf(mv[n][j], top[j] + vexp);
+          ref[j] = m1 > -INFINITY ? m1 : 0.f;
+          refv[j] = mv1 > -INFINITY ? mv1 : 0.f;
+          if (m1 > m[n][j]) { l[n][j] *= fast_exp2(m[n][j] - ref[j]); m[n][j] = m1; }
+          grown |= mv1 > mv[n][j];
+        }
+        if (__any_sync(0xffffffffu, grown)) {
+          float f[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            f[j] = fast_exp2(mv[n][j] - refv[j]);   // 0 where nothing has been added yet
+            mv[n][j] = fmaxf(mv[n][j], top[j] + vexp);
+            if (!(mv[n][j] > -INFINITY)) f[j] = 1.f;
+          }
+#pragma unroll
+          for (int c = 0; c < kSteps; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[n][c][e] *= f[e & 1];
+        }
+        float w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          l[n][e & 1] += fast_exp2(v[e] - ref[e & 1]);
+          w[e] = fast_exp2(v[e] + vexp - refv[e & 1]);
+        }
+        const uint32_t lo = half_pair(w[0], w[1]), hi = half_pair(w[2], w[3]);
+        pf[0][n][0] = transpose8x8(lo);   // head g, rows 2 t and 2 t + 1
+        pf[0][n][1] = transpose8x8(hi);   // rows 2 t + 8 and 2 t + 9
+        if constexpr (kTerms == 2) {
+          pf[kTerms - 1][n][0] = transpose8x8(half_rest(w[0], w[1], lo));
+          pf[kTerms - 1][n][1] = transpose8x8(half_rest(w[2], w[3], hi));
+        }
+      }
+      // ---- O^T += V^T P^T: 16 dims x 8 heads a tile; row g is dim 16 c + 2 g, row g + 8 the one after it ----
+#pragma unroll
+      for (int c = 0; c < kSteps; c += 2) {
+        uint32_t r[4];
+        ldsm4_t(r, vb + (((c + (lane >> 4)) ^ lxor) << 4));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] ^= 0x80808080u;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t a0 = codes_f16<0x4240>(r[2 * j]), a1 = codes_f16<0x4341>(r[2 * j]);
+          const uint32_t a2 = codes_f16<0x4240>(r[2 * j + 1]), a3 = codes_f16<0x4341>(r[2 * j + 1]);
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int term = 0; term < kTerms; ++term) mma_f16(acc[n][c + j], a0, a1, a2, a3, pf[term][n][0], pf[term][n][1]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) ca_arrive(&empty[stage]);
+      if (++stage == L::kStages) { stage = 0; parity ^= 1; }
+    }
+    // ---- the four warps' shares become the segment's partial ----
+    if (!ok) {
+      *fail = 1;
+      if (lane == 0 && p.status) atomicOr(p.status, ST3_DEV_COPY_TIMEOUT);
+    }
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l[n][j] += __shfl_xor_sync(0xffffffffu, l[n][j], o);
+        if (g == 0) {
+          float* dst = s_ml + (warp * kCaHeads + n * 8 + 2 * t + j) * 3;
+          dst[0] = m[n][j]; dst[1] = mv[n][j]; dst[2] = l[n][j];
+        }
+      }
+    }
+    if (ca_any_failed(!ok)) return;   // one verdict for the four warps: the barriers below count on all of them
+    const size_t slot = (size_t)blockIdx.x + (size_t)b * pairs + pair;
+    float* out_acc = p.part_acc + slot * p.pitch * D;
+    float* out_ml = p.part_ml + slot * p.pitch * 3;
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      float f[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float all = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kCaConsumers; ++w) all = fmaxf(all, s_ml[(w * kCaHeads + n * 8 + 2 * t + j) * 3 + 1]);
+        f[j] = all > -INFINITY ? fast_exp2(mv[n][j] - all) : 0.f;
+      }
+      float* dst = s_red + (size_t)warp * 8 * L::kPitch;
+#pragma unroll
+      for (int c = 0; c < kSteps; ++c)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          *reinterpret_cast<float2*>(dst + (2 * t + j) * L::kPitch + 16 * c + 2 * g) = make_float2(acc[n][c][j] * f[j], acc[n][c][2 + j] * f[j]);
+      asm volatile("bar.sync 1, %0;" ::"n"(kCaConsumers * 32) : "memory");
+      for (int e = tid; e < 8 * D; e += kCaConsumers * 32) {
+        const int h = e / D, d = e - h * D;
+        if (n * 8 + h < heads) {
+          float sum = 0.f;
+#pragma unroll
+          for (int w = 0; w < kCaConsumers; ++w) sum += s_red[(w * 8 + h) * L::kPitch + d];
+          out_acc[(n * 8 + h) * D + d] = sum;
+        }
+      }
+      if (tid < 8 && n * 8 + tid < heads) {
+        float a = -INFINITY, av = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kCaConsumers; ++w) {
+          const float* src = s_ml + (w * kCaHeads + n * 8 + tid) * 3;
+          a = fmaxf(a, src[0]);
+          av = fmaxf(av, src[1]);
+        }
+        const float ref = a > -INFINITY ? a : 0.f;
+#pragma unroll
+        for (int w = 0; w < kCaConsumers; ++w) {
+          const float* src = s_ml + (w * kCaHeads + n * 8 + tid) * 3;
+          sum += src[2] * fast_exp2(src[0] - ref);
+        }
+        float* dst3 = out_ml + (n * 8 + tid) * 3;
+        dst3[0] = a; dst3[1] = av; dst3[2] = sum;
+      }
+      asm volatile("bar.sync 1, %0;" ::"n"(kCaConsumers * 32) : "memory");
+    }
+    x += i1 - i0;
+  }
+}
+
+// Joins the partials of a (sequence, key/value head) into the output (grid y = 0 .. passes - 1), and adds the probabilities
+// of its rows to their weights (the other y, kCaChunk rows each).
+template <typename T, int D>
+__global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const CacheAttendParams p) {
+  __shared__ int s_sum[2][kCaMergeThreads / 32];
+  __shared__ float s_ref[128], s_inv[128];
+  __shared__ float s_acc[kCaMergeThreads / 32][D];
+  pdl_wait();
+  pdl_next();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x;
+  const int b = bh / p.c.heads, head = bh - b * p.c.heads, pairs = p.c.heads * p.passes;
+  const int held = clamp_rows(p.held[b], p.c.cap), nb = (held + kBlockRows - 1) / kBlockRows;
+  const bool weigh = (int)blockIdx.y >= p.passes;
+  const int row0 = ((int)blockIdx.y - p.passes) * kCaChunk;
+  if (weigh && row0 >= held) return;
+  if (nb == 0) {
+    T* out = static_cast<T*>(p.out) + ((size_t)bh * p.group + blockIdx.y * kCaHeads) * D;
+    const int n = min(p.group - (int)blockIdx.y * kCaHeads, kCaHeads) * D;
+    for (int i = tid; i < n; i += kCaMergeThreads) store_out(out + i, 0.f);
+    return;
+  }
+  int all = 0, below = 0;
+  for (int i = tid; i < p.c.batch; i += kCaMergeThreads) {
+    const int n = blocks_of(p, i);
+    all += n;
+    if (i < b) below += n;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    all += __shfl_xor_sync(0xffffffffu, all, o);
+    below += __shfl_xor_sync(0xffffffffu, below, o);
+  }
+  if (lane == 0) { s_sum[0][warp] = all; s_sum[1][warp] = below; }
+  __syncthreads();
+  all = below = 0;
+#pragma unroll
+  for (int w = 0; w < kCaMergeThreads / 32; ++w) { all += s_sum[0][w]; below += s_sum[1][w]; }
+  const int total = all * pairs, grid = min(p.grid, total);
+  constexpr int kWarps8 = kCaMergeThreads / 32;
+  if (!weigh) {
+    const int pass = blockIdx.y, pair = head * p.passes + pass;
+    const int heads = min(p.group - pass * kCaHeads, kCaHeads);
+    const int x = (below * pairs) + pair * nb;
+    const int c0 = run_of(total, x, grid), c1 = run_of(total, x + nb - 1, grid);
+    const size_t slot0 = (size_t)b * pairs + pair;
+    // warps to a head, and the segments that each of them takes
+    const int split = heads >= kWarps8 ? 1 : kWarps8 / heads;
+    for (int h = warp / split; h < (heads + kWarps8 - 1) / kWarps8 * kWarps8; h += kWarps8 / split) {
+      const bool live = h < heads && warp / split < kWarps8 / split;
+      const int part = warp % split;
+      float a = -INFINITY, av = -INFINITY, sum = 0.f;
+      float o[D / 32];
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+      if (live) {
+        for (int c = c0 + lane; c <= c1; c += 32) {
+          const float* ml = p.part_ml + ((slot0 + c) * p.pitch + h) * 3;
+          a = fmaxf(a, ml[0]);
+          av = fmaxf(av, ml[1]);
+        }
+        a = warp_max(a);
+        av = warp_max(av);
+        const float ref = a > -INFINITY ? a : 0.f, refv = av > -INFINITY ? av : 0.f;
+        for (int c = c0 + lane; c <= c1; c += 32) {
+          const float* ml = p.part_ml + ((slot0 + c) * p.pitch + h) * 3;
+          sum += ml[2] * fast_exp2(ml[0] - ref);
+        }
+        sum = warp_sum(sum);
+#pragma unroll 4
+        for (int c = c0 + part; c <= c1; c += split) {
+          const float f = fast_exp2(p.part_ml[((slot0 + c) * p.pitch + h) * 3 + 1] - refv);
+          const float* src = p.part_acc + ((slot0 + c) * p.pitch + h) * D + lane * (D / 32);
+          if constexpr (D == 128) {
+            const float4 v = *reinterpret_cast<const float4*>(src);
+            o[0] += v.x * f; o[1] += v.y * f; o[D / 32 - 2] += v.z * f; o[D / 32 - 1] += v.w * f;
+          } else {
+            const float2 v = *reinterpret_cast<const float2*>(src);
+            o[0] += v.x * f; o[1] += v.y * f;
+          }
+        }
+        // sums relative to 2^refv over a denominator relative to 2^ref
+        const float inv = fast_exp2(refv - ref) / sum;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o[e] *= inv;
+      }
+      if (split > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) s_acc[warp][lane * (D / 32) + e] = o[e];
+        __syncthreads();
+        if (live && part == 0)
+          for (int w = 1; w < split; ++w)
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) o[e] += s_acc[warp + w][lane * (D / 32) + e];
+      }
+      if (live && part == 0) {
+        T* dst = static_cast<T*>(p.out) + ((size_t)bh * p.group + pass * kCaHeads + h) * D + lane * (D / 32);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) store_out(dst + e, o[e]);
+      }
+      if (split > 1) break;   // one round covers all heads
+    }
+    return;
+  }
+  // ---- weights ----
+  for (int h0 = 0; h0 < p.group; h0 += 128) {
+    __syncthreads();
+    for (int h = h0 + warp; h < min(p.group, h0 + 128); h += kWarps8) {
+      const int pass = h / kCaHeads, pair = head * p.passes + pass;
+      const int x = (below * pairs) + pair * nb;
+      const int c0 = run_of(total, x, grid), c1 = run_of(total, x + nb - 1, grid);
+      const size_t slot0 = (size_t)b * pairs + pair;
+      float a = -INFINITY, sum = 0.f;
+      for (int c = c0 + lane; c <= c1; c += 32) a = fmaxf(a, p.part_ml[((slot0 + c) * p.pitch + h - pass * kCaHeads) * 3]);
+      a = warp_max(a);
+      const float ref = a > -INFINITY ? a : 0.f;
+      for (int c = c0 + lane; c <= c1; c += 32) {
+        const float* ml = p.part_ml + ((slot0 + c) * p.pitch + h - pass * kCaHeads) * 3;
+        sum += ml[2] * fast_exp2(ml[0] - ref);
+      }
+      sum = warp_sum(sum);
+      if (lane == 0) { s_ref[h - h0] = ref; s_inv[h - h0] = 1.f / sum; }
+    }
+    __syncthreads();
+    const int n = min(p.group - h0, 128);
+    for (int r = row0 + tid; r < min(row0 + kCaChunk, held); r += kCaMergeThreads) {
+      const float* src = p.logits + ((size_t)bh * p.c.cap + r) * p.group + h0;
+      const size_t at = (size_t)bh * p.c.cap + r;
+      float sum = 0.f;
+      for (int j = 0; j < n; ++j) sum += fast_exp2(src[j] - s_ref[j]) * s_inv[j];
+      p.weights_out[at] = (h0 ? p.weights_out[at] : p.weights_in[at]) + sum;
+    }
+  }
+}
+
+}  // namespace
+
+#endif  // ST3_CACHE_ATTEND_CUH_

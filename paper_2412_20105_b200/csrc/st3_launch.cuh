@@ -1,0 +1,46 @@
+// Host helpers of the context-free entry points; included by the .cu files that launch kernels themselves.
+#ifndef ST3_LAUNCH_CUH_
+#define ST3_LAUNCH_CUH_
+#include "st3.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+namespace {
+
+// A launch that may be set up while the one ahead of it in the stream still runs; the kernel waits for it itself.
+template <typename... P, typename... A>
+st3_status launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const A&... args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? ST3_OK : ST3_ERR_CUDA;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder of tensor maps; null if it does not offer one.  Looked up once (initialisation of a local static is
+// thread-safe).
+inline EncodeTiledFn tensor_map_encoder() {
+  static const EncodeTiledFn encode = [] {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess ||
+        qres != cudaDriverEntryPointSuccess)
+      fn = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(fn);
+  }();
+  return encode;
+}
+
+}  // namespace
+#endif  // ST3_LAUNCH_CUH_
