@@ -293,6 +293,44 @@ st3_status st3_prefill_attend_kept(const void* q, const void* k, const void* v, 
 st3_status st3_attend_noalloc(const void* q, const void* k, const void* v, void* out, int32_t num_heads,
                               int32_t num_rows, int32_t head_dim, int32_t dtype, void* cuda_stream);
 
+/* ---- Prompts packed one behind the other, with grouped heads ------------------------------------------------------
+ *
+ * A batch of prompts of different lengths is one tensor of tokens; sequence s is the rows cu[s] .. cu[s+1]-1.  Query
+ * head h reads key/value head h / (num_heads / num_kv_heads).  Neither call needs a context or a workspace. */
+typedef struct {
+  int32_t num_seqs;      /* sequences (0 allowed)                                                   */
+  int32_t total;         /* tokens of all sequences = cu[num_seqs] (0 allowed)                      */
+  int32_t num_heads;     /* query heads, a multiple of num_kv_heads                                 */
+  int32_t num_kv_heads;
+  int32_t head_dim;      /* 64 or 128                                                               */
+  int32_t dtype;         /* ST3_BF16                                                                */
+  /* elements from one token to the next and from one head to the next, multiples of 8: [token][head][D],
+   * [head][token][D] and slices of a fused projection are all possible; the D elements lie side by side */
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  int64_t out_token_stride, out_head_stride;
+} st3_packed;
+
+/* Causal attention inside each sequence (Eq. 2: A = Softmax((Q K^T + M)/sqrt(D)), out = A V) on the tcgen05 tensor
+ * cores.
+ *   cu          dev int32 [num_seqs + 1], ascending from 0 to total
+ *   out         dev, like q with its own strides
+ *   lse         dev fp32 [num_heads][total], may be NULL: log sum_j exp(q_i . k_j / sqrt(D)) of every row
+ *   dev_status  dev int, may be NULL: ST3_DEV_COPY_TIMEOUT as in st3_prefill_attend, ST3_DEV_RANGE if cu is not what it
+ *               should be (the sequences concerned are skipped)
+ * A value row that is not finite reaches the rows of its own sequence from up to 127 tokens before it on (their
+ * probability of 0 times Inf), but no other sequence. */
+st3_status st3_packed_attend(const st3_packed* p, const void* q, const void* k, const void* v, const int32_t* cu,
+                             void* out, float* lse, int* dev_status, void* cuda_stream);
+
+/* The attention weight each token of the packed prompts has received: for every sequence s, key/value head g and token j
+ *   weights[s][g][j] = sum over the heads of the group and over queries i >= j of exp(q_i . k_j / sqrt(D) - lse_i),
+ * over all queries (window = 0) or the last `window` of the sequence.  lse is st3_packed_attend's; only k, q and lse are
+ * read (v's and out's strides are ignored).
+ *   weights     dev fp32 [num_seqs][num_kv_heads][capacity], e.g. st3_cache.weights; places past a sequence's end are
+ *               left as they were.  A sequence longer than capacity sets ST3_DEV_RANGE and is skipped. */
+st3_status st3_packed_weights(const st3_packed* p, const void* q, const void* k, const float* lse, const int32_t* cu,
+                              float* weights, int32_t capacity, int32_t window, int* dev_status, void* cuda_stream);
+
 /* ---- A cache of grouped heads held in 8 bits -----------------------------------------------------------------------
  *
  * One layer's keys and values, with the tokens' positions and the attention weight they have accumulated.  Rows

@@ -25,7 +25,7 @@ EXPORTS = ["st3_schedule_count", "st3_workspace_size", "st3_create", "st3_prefil
            "st3_decode_step_host", "st3_prefill_select_host", "st3_host_sync", "st3_get_kept", "st3_get_rows", "st3_get_status", "st3_rows_held",
            "st3_set_overlap", "st3_profile_enable", "st3_profile_read", "st3_launch_count", "st3_status_string", "st3_destroy",
            "st3_attend_noalloc", "st3_prefill_attend", "st3_prefill_attend_kept",
-           "st3_cache_store", "st3_cache_attend_workspace", "st3_cache_attend", "st3_cache_evict_workspace",
+           "st3_packed_attend", "st3_packed_weights", "st3_cache_store", "st3_cache_attend_workspace", "st3_cache_attend", "st3_cache_evict_workspace",
            "st3_cache_evict", "st3_cache_rows"]
 
 
@@ -35,6 +35,12 @@ class Config(C.Structure):
         "num_layers", "num_heads", "head_dim", "dtype", "batch", "sys_len", "num_visual", "max_text_len",
         "max_decode_steps", "first_prune_layer", "stride", "first_ratio_bp", "step_ratio_bp", "anneal",
         "disable_trim", "rows_per_chunk", "static_rank", "stage_shared", "host_prefill")] + [("lazy_mask", C.c_uint64), ("tau", C.c_double), ("sigma", C.c_double)]
+
+
+class PackedDesc(C.Structure):
+    """Mirror of `st3_packed` (include/st3.h)."""
+    _fields_ = [(n, C.c_int32) for n in ("num_seqs", "total", "num_heads", "num_kv_heads", "head_dim", "dtype")] + [
+        (f"{t}_{n}_stride", C.c_int64) for t in ("q", "k", "v", "out") for n in ("token", "head")]
 
 
 class CacheDesc(C.Structure):
@@ -91,6 +97,9 @@ def load():
     lib.st3_prefill_attend.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]
     lib.st3_prefill_attend_kept.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, i32, vp]
     cp, szp = C.POINTER(CacheDesc), C.POINTER(C.c_size_t)
+    pp = C.POINTER(PackedDesc)
+    lib.st3_packed_attend.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.st3_packed_weights.argtypes = [pp, vp, vp, vp, vp, vp, i32, i32, vp, vp]
     lib.st3_cache_store.argtypes = [cp, vp, vp, i32, i64, i64, i64, i64, vp, i32, vp, vp, vp, vp]
     lib.st3_cache_attend_workspace.argtypes = [cp, i32, i32, szp]
     lib.st3_cache_attend.argtypes = [cp, vp, vp, i32, i32, vp, vp, vp, vp, C.c_size_t, vp, vp]
@@ -246,6 +255,16 @@ def st3_attend_noalloc(q, k, v, out, num_heads, num_rows, head_dim, dtype, strea
     _check(load().st3_attend_noalloc(q, k, v, out, num_heads, num_rows, head_dim, dt, stream), "st3_attend_noalloc")
 
 
+def st3_packed_attend(desc, q, k, v, cu, out, lse=None, dev_status=None, stream=0):
+    """desc is a PackedDesc; the rest device addresses."""
+    _check(load().st3_packed_attend(C.byref(desc), q, k, v, cu, out, lse, dev_status, stream), "st3_packed_attend")
+
+
+def st3_packed_weights(desc, q, k, lse, cu, weights, capacity, window=0, dev_status=None, stream=0):
+    _check(load().st3_packed_weights(C.byref(desc), q, k, lse, cu, weights, capacity, window, dev_status, stream),
+           "st3_packed_weights")
+
+
 def st3_cache_store(cache, k, v, dtype, k_strides, v_strides, cu, total, start=None, pos=None, dev_status=None, stream=0):
     """cache is a CacheDesc; k_strides and v_strides are (token, head) strides in elements; the rest device addresses."""
     _check(load().st3_cache_store(C.byref(cache), k, v, dtype, *k_strides, *v_strides, cu, total, start, pos, dev_status,
@@ -317,6 +336,46 @@ def _rows_view(t, heads, dim, dtype, device, what):
     if t.stride(2) != 1:
         raise ValueError(f"{what}: the elements of a head have to lie side by side")
     return t.data_ptr(), (t.stride(0), t.stride(1))
+
+
+def _packed(q, k, cu):
+    import torch
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k: tensors of [tokens, heads, dim] are needed")
+    total, heads, dim = q.shape
+    qp, qs = _rows_view(q, heads, dim, q.dtype, q.device, "q")
+    kp, ks = _rows_view(k, k.shape[1], dim, q.dtype, q.device, "k")
+    if k.shape[0] != total:
+        raise ValueError("q and k have different numbers of tokens")
+    if cu.dim() != 1 or cu.numel() < 1:
+        raise ValueError("cu: [sequences + 1] is needed")
+    desc = PackedDesc(cu.numel() - 1, total, heads, k.shape[1], dim, _dtype_of(q), *qs, *ks, *ks, *qs)
+    return desc, qp, kp, _dense(cu, cu.shape, torch.int32, q.device, "cu")
+
+
+def packed_attend(q, k, v, cu, out, lse=None, status=None):
+    """Causal attention of packed prompts: q, out [tokens, heads, dim], k, v [tokens, kv heads, dim], lse [heads, tokens]."""
+    import torch
+    desc, qp, kp, cup = _packed(q, k, cu)
+    vp, (desc.v_token_stride, desc.v_head_stride) = _rows_view(v, k.shape[1], q.shape[2], q.dtype, q.device, "v")
+    op, (desc.out_token_stride, desc.out_head_stride) = _rows_view(out, q.shape[1], q.shape[2], q.dtype, q.device, "out")
+    if v.shape[0] != q.shape[0] or out.shape[0] != q.shape[0]:
+        raise ValueError("q, v and out have different numbers of tokens")
+    st3_packed_attend(desc, qp, kp, vp, cup, op,
+                      None if lse is None else _dense(lse, (q.shape[1], q.shape[0]), torch.float32, q.device, "lse"),
+                      None if status is None else _dense(status, (1,), torch.int32, q.device, "status"), _stream_of(q))
+
+
+def packed_weights(q, k, lse, cu, weights, window=0, status=None):
+    """What each token has received from all queries, or from the last `window`: weights [sequences, kv heads, capacity]."""
+    import torch
+    desc, qp, kp, cup = _packed(q, k, cu)
+    if weights.dim() != 3:
+        raise ValueError("weights: [sequences, kv heads, capacity] is needed")
+    shape = (desc.num_seqs, desc.num_kv_heads, weights.shape[2])
+    st3_packed_weights(desc, qp, kp, _dense(lse, (q.shape[1], q.shape[0]), torch.float32, q.device, "lse"), cup,
+                       _dense(weights, shape, torch.float32, q.device, "weights"), weights.shape[2], window,
+                       None if status is None else _dense(status, (1,), torch.int32, q.device, "status"), _stream_of(q))
 
 
 class Cache:

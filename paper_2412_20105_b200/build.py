@@ -7,10 +7,11 @@ import subprocess
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libst3.so")
-SOURCES = [os.path.join(PKG, "csrc", f) for f in ("st3.cu", "st3_prefill.cu", "st3_cache.cu")]
+SOURCES = [os.path.join(PKG, "csrc", f) for f in ("st3.cu", "st3_prefill.cu", "st3_packed.cu", "st3_cache.cu")]
 HEADERS = [os.path.join(ROOT, "include", "st3.h")] + [
     os.path.join(PKG, "csrc", f) for f in (
-        "st3_common.cuh", "st3_attend.cuh", "st3_finish.cuh", "st3_launch.cuh", "st3_cache_attend.cuh")]
+        "st3_common.cuh", "st3_attend.cuh", "st3_finish.cuh", "st3_launch.cuh", "st3_tensor.cuh",
+        "st3_cache_attend.cuh")]
 
 
 def needs_build() -> bool:

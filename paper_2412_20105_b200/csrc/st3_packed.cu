@@ -1,0 +1,846 @@
+// Prompts of different lengths packed one behind the other, with grouped heads: causal attention, and the attention weight
+// that every token has received.  Both run on the tcgen05 tensor cores with accumulators in tensor memory.
+//
+// Work items are two tiles of 128 rows that read the same other operand, so that every tile that comes through the ring
+// feeds two tiles of MMAs: for the attention 128 queries of two heads of one group (or, where a group has an odd number
+// of heads, 256 queries of one head) against key/value tiles of 128 rows; for the weights 256 keys of a key/value
+// head against tiles of 128 queries.  A block per SM is persistent: the first item is its block index, the others are block
+// indices that it takes from the hardware's queue (cluster launch control), so that items of very different lengths
+// spread without a counter in memory and the next item's loads run under the end of this one.
+//
+// Items need no table either: sequence s has the numbers cu[s]/R + s and on (R rows an item), which are at least as many as
+// the ceil(n/R) that it needs.  The number of an item says nothing of its sequence's length; numbers without rows are
+// passed over.
+//
+// Roles: warps 0-3 and 4-7 own one tile each, a row (= tensor memory lane) per thread; warp 8 issues the MMAs; warp 9 takes
+// items, decodes them and issues the TMA loads.  Every wait is bounded, and a wait that runs out ends the block's others.
+#include "st3_common.cuh"
+#include "st3_launch.cuh"
+#include "st3_tensor.cuh"
+
+namespace {
+
+constexpr int kPkThreads = 320;
+constexpr int kPkRows = 128;                 // rows of a tile
+constexpr int kBox = kPkRows * 128;          // one TMA box: 128 rows x 64 bf16
+constexpr uint32_t kPkTmem = 512;
+constexpr uint32_t kIdescScores = kIdescBase | ((128u >> 3) << 17);   // N = 128, both operands K-major
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct PackedParams {
+  const int* cu;
+  void* out;
+  float* lse;
+  const float* lse_in;
+  float* weights;
+  int* status;
+  long long out_token_stride, out_head_stride;
+  int num_seqs, total, heads, kv_heads, group;
+  int pairs;       // items of one number: head pairs, or heads where an item is 256 queries of one
+  int items;
+  int by_heads;    // an item's tiles are two heads (else two runs of 128 queries)
+  int wide_out;    // rows of the output start on 32 bytes
+  int capacity, window;
+};
+
+struct PkItem {
+  int stop;
+  int row;        // first token of the sequence in the packed tensor
+  int len;
+  int seq;
+  int head[2];    // of the two tiles
+  int first[2];   // first row of the two tiles inside the sequence
+  int steps[2];   // tiles of the other operand
+  int begin;      // weights: first query that counts
+};
+
+struct PkShared {
+  uint64_t full[8], empty[8];           // ring of the other operand
+  uint64_t own, own_free;               // the item's own two tiles
+  uint64_t scores[4];                   // S is complete (attention: one per tile; weights: two per tile)
+  uint64_t taken[4];                    // attention: P is in tensor memory, by halves; weights: S has been read
+  uint64_t done[2];                     // the last P V of a tile
+  uint64_t ready[2], read[2];           // items
+  uint64_t next;                        // answer of the queue
+  uint4 answer;
+  PkItem item[2];
+  uint32_t tmem;
+  int fail;
+};
+
+template <int D>
+struct PkLayout {
+  static constexpr int kBoxes = D / 64;
+  static constexpr int kTile = kBoxes * kBox;
+  static constexpr int kStages = D == 128 ? 5 : 8;
+  static constexpr int kRing = 2 * kTile;
+  static constexpr int kShared = kRing + kStages * kTile;
+  static constexpr int kLse = kShared + 768;                       // weights: two buffers of 128 sums for each tile
+  static constexpr int kTotal = kShared + 768;
+  static constexpr int kTotalWeights = kLse + 2 * 2 * kPkRows * 4;
+};
+static_assert(sizeof(PkShared) <= 768, "PkShared must fit its slot");
+static_assert(PkLayout<128>::kTotalWeights <= 227 * 1024, "shared memory");
+
+// Bounded wait that also ends when another role of the block has given up.
+__device__ __forceinline__ bool pk_wait(uint64_t* bar, uint32_t parity, volatile int* fail) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (*fail || clock64() - t0 > kWaitCycles) return false;
+  return true;
+}
+__device__ __forceinline__ bool pk_wait_warp(uint64_t* bar, uint32_t parity, volatile int* fail) {
+  return __all_sync(0xffffffffu, pk_wait(bar, parity, fail));
+}
+
+__device__ __forceinline__ void take_next(void* answer, uint64_t* bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)),
+               "r"(smem_u32(bar))
+               : "memory");
+}
+// The block index that was taken, or -1 when the queue is empty.
+__device__ __forceinline__ int taken_index(const void* answer) {
+  uint32_t got, x;
+  asm volatile(
+      "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t.reg .b32 y, z, w;\n\t"
+      "ld.shared.b128 r, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "mov.u32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, r;\n\t}"
+      : "=r"(got), "=r"(x)
+      : "r"(smem_u32(answer))
+      : "memory");
+  return got ? (int)x : -1;
+}
+
+template <int D>
+__device__ __forceinline__ void load_tile(unsigned char* dst, const CUtensorMap* map, int head, int row, uint64_t* bar) {
+#pragma unroll
+  for (int x = 0; x < PkLayout<D>::kBoxes; ++x) tma_load_3d(dst + x * kBox, map, x * 64, head, row, bar);
+}
+
+// The sequence of item number `slot` (R rows an item): how many sequences start at or below it, less one.  A whole warp.
+__device__ __forceinline__ int seq_of(const int* cu, int num_seqs, int rows, int slot) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = num_seqs;
+  while (n > 0) {   // sequences lo .. lo + n - 1 are left to look at
+    const int step = (n + 31) / 32, b = lo + lane * step;
+    const bool below = b < lo + n && cu[b] / rows + b <= slot;
+    const int c = __popc(__ballot_sync(0xffffffffu, below));
+    if (c == 0) break;
+    const int base = lo + (c - 1) * step;
+    if (step == 1) { lo = base; break; }
+    n = min(step, lo + n - base);
+    lo = base;
+  }
+  return lo;
+}
+
+// Where sequence b lies; false (and reported) if cu is not ascending inside [0, total].
+__device__ __forceinline__ bool seq_rows(const PackedParams& p, int b, int& row, int& len) {
+  row = p.cu[b];
+  len = p.cu[b + 1] - row;
+  const bool ok = row >= 0 && len >= 0 && row <= p.total - len;
+  if (!ok && p.status && (threadIdx.x & 31) == 0) atomicOr(p.status, ST3_DEV_RANGE);
+  return ok;
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// The barriers, the tensor memory and the start of a block; false if its shared memory is not where it must be.
+template <int D>
+__device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int* status, int taken_count) {
+  if (smem_u32(smem) & 1023u) {   // the swizzle assumes aligned tiles: reported, not used
+    if (threadIdx.x == 0 && status) atomicOr(status, ST3_DEV_RANGE);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    return false;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < PkLayout<D>::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+    mbar_init(&sh.own, 1);
+    mbar_init(&sh.own_free, 1);
+    for (int i = 0; i < 4; ++i) { mbar_init(&sh.scores[i], 1); mbar_init(&sh.taken[i], taken_count); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.done[i], 1); mbar_init(&sh.ready[i], 1); mbar_init(&sh.read[i], 9); }
+    mbar_init(&sh.next, 1);
+    sh.fail = 0;
+    mbar_fence_init();
+  }
+  __syncthreads();
+  if (threadIdx.x >> 5 == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(kPkTmem) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  return true;
+}
+__device__ __forceinline__ void pk_end(PkShared& sh, uint32_t tmem) {
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x >> 5 == 8)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kPkTmem) : "memory");
+}
+
+// Waits for an item and copies it; false when there is none left (or a wait ran out, then `fail` is set).
+__device__ __forceinline__ bool pk_item(PkShared& sh, int& slot, uint32_t& phase, PkItem& it) {
+  if (!pk_wait_warp(&sh.ready[slot], phase, &sh.fail)) { *(volatile int*)&sh.fail = 1; return false; }
+  it = sh.item[slot];
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive_cta(&sh.read[slot]);
+  if (++slot == 2) { slot = 0; phase ^= 1; }
+  return !it.stop;
+}
+
+// The MMA warp's end where a wait has run out: what it has issued (a microsecond's work) ends before tensor memory is given
+// back.
+__device__ __forceinline__ void pk_give_up(PkShared& sh, int* status) {
+  *(volatile int*)&sh.fail = 1;
+  if ((threadIdx.x & 31) == 0 && status) atomicOr(status, ST3_DEV_COPY_TIMEOUT);
+  const long long t0 = clock64();
+  while (clock64() - t0 < 2000000) {}
+  __syncwarp();
+}
+
+// A barrier of the four warps of a tile that tells each of them whether any has failed.
+__device__ __forceinline__ bool pk_any_failed(int tile, bool failed) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)failed), "r"(1 + tile)
+      : "memory");
+  return any != 0;
+}
+
+// The loader's loop over items, the same for both kernels: `decode(index, item)` fills an item (false: nothing to do) and
+// `load(item)` brings its tiles.
+template <typename Decode, typename Load>
+__device__ __forceinline__ void pk_loader(PkShared& sh, int* status, Decode&& decode, Load&& load) {
+  const int lane = threadIdx.x & 31;
+  int index = blockIdx.x, slot = 0;
+  uint32_t phase = 1, answer = 0;
+  bool ok = true;
+  while (ok) {
+    if (lane == 0) {
+      mbar_expect_tx(&sh.next, 16);
+      take_next(&sh.answer, &sh.next);
+    }
+    PkItem it;
+    if (decode(index, it)) {
+      ok = pk_wait_warp(&sh.read[slot], phase, &sh.fail);
+      if (ok) {
+        if (lane == 0) { it.stop = 0; sh.item[slot] = it; mbar_arrive_cta(&sh.ready[slot]); }
+        __syncwarp();
+        if (++slot == 2) { slot = 0; phase ^= 1; }
+        ok = load(it);
+      }
+    }
+    // the answer is waited for also where the block gives up: it is written into this block's shared memory
+    if (!pk_wait_warp(&sh.next, answer, &sh.fail) && !pf_wait_warp(&sh.next, answer)) { ok = false; break; }
+    answer ^= 1;
+    index = taken_index(&sh.answer);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // read before the next answer may be written
+    __syncwarp();
+    if (index < 0) break;
+  }
+  if (ok) ok = pk_wait_warp(&sh.read[slot], phase, &sh.fail);
+  if (lane == 0) {
+    if (!ok) {
+      *(volatile int*)&sh.fail = 1;
+      if (status) atomicOr(status, ST3_DEV_COPY_TIMEOUT);
+    }
+    sh.item[slot].stop = 1;
+    mbar_arrive_cta(&sh.ready[slot]);
+  }
+  __syncwarp();
+}
+
+// A ring's place: stage and parity of its next use.
+template <int kStages>
+struct Ring {
+  int stage = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step() { if (++stage == kStages) { stage = 0; phase ^= 1; } }
+};
+
+// Copies still in flight when the loader leaves: the last use of every stage, and the item's own tiles.
+template <int kStages>
+__device__ __forceinline__ void pk_settle(PkShared& sh, int issued, int owned) {
+  for (int u = max(0, issued - kStages); u < issued; ++u) pf_wait(&sh.full[u % kStages], (u / kStages) & 1);
+  if (owned > 0) pf_wait(&sh.own, (owned - 1) & 1);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Causal attention.
+//   S = Q K^T (128 x 128, D/16 MMAs of K = 16), P = exp2(S - ref) as bf16 over the first half of its S, O += P V.
+// The tensor pipe runs PV_A(j) S_A(j+1) | PV_B(j) S_B(j+1) | ...: while one tile's softmax runs, the other tile's two
+// products do.  P goes back in two halves of 64 keys, the first of which P V starts on while the second is computed.  `ref`
+// follows a row's maximum only when that has grown by 2^32: bf16 and fp32 have the range for it and lose no bits, and
+// O is then hardly ever rescaled.  S(j) complete says that P V(j-1) is, which came before it in the pipe.
+// ------------------------------------------------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(kPkThreads, 1)
+st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                         const __grid_constant__ CUtensorMap map_v, const PackedParams p) {
+  using L = PkLayout<D>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
+  if (!pk_begin<D>(smem, sh, p.status, 4)) return;
+  const uint32_t tmem = sh.tmem;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int* fail = &sh.fail;
+  const int rows = p.by_heads ? kPkRows : 2 * kPkRows;
+
+  if (warp == 9) {
+    // ===================== loader =====================
+    Ring<L::kStages> ring;
+    int issued = 0, owned = 0;
+    pk_loader(
+        sh, p.status,
+        [&](int index, PkItem& it) {
+          const int number = index / p.pairs, pair = index - number * p.pairs;
+          const int slot = p.items / p.pairs - 1 - number;    // a sequence's last rows, the longest items, first
+          const int b = seq_of(p.cu, p.num_seqs, rows, slot);
+          if (!seq_rows(p, b, it.row, it.len)) return false;
+          const int rank = slot - (p.cu[b] / rows + b);
+          if (rank < 0 || rank >= (it.len + rows - 1) / rows) return false;
+          it.seq = b;
+          it.head[0] = p.by_heads ? 2 * pair : pair;
+          it.head[1] = p.by_heads ? 2 * pair + 1 : pair;
+          it.first[0] = rank * rows;
+          it.first[1] = it.first[0] + rows - kPkRows;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) it.steps[x] = it.first[x] < it.len ? it.first[x] / kPkRows + 1 : 0;
+          it.begin = 0;
+          return true;
+        },
+        [&](const PkItem& it) {
+          bool ok = pk_wait_warp(&sh.own_free, (owned & 1) ^ 1, fail);
+          if (!ok) return false;
+          if (lane == 0) {
+            mbar_expect_tx(&sh.own, 2 * L::kTile);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) load_tile<D>(smem + x * L::kTile, &map_q, it.head[x], it.row + it.first[x], &sh.own);
+          }
+          ++owned;
+          const int n = max(it.steps[0], it.steps[1]), kv = it.head[0] / p.group;
+          for (int j = 0; j < 2 * n && ok; ++j) {   // K(0) V(0) K(1) V(1) ...
+            ok = pk_wait_warp(&sh.empty[ring.stage], ring.phase ^ 1, fail);
+            if (!ok) break;
+            if (lane == 0) {
+              mbar_expect_tx(&sh.full[ring.stage], L::kTile);
+              load_tile<D>(smem + L::kRing + ring.stage * L::kTile, j & 1 ? &map_v : &map_k, kv, it.row + (j >> 1) * kPkRows, &sh.full[ring.stage]);
+            }
+            __syncwarp();
+            ++issued;
+            ring.step();
+          }
+          return ok;
+        });
+    if (lane == 0) pk_settle<L::kStages>(sh, issued, owned);
+    __syncwarp();
+  } else if (warp == 8) {
+    // ===================== MMA =====================
+    constexpr uint32_t kIdescOut = kIdescBase | (((uint32_t)D >> 3) << 17) | (1u << 16);   // N = D, V MN-major
+    const uint32_t own_lo = desc_lo(smem_u32(smem), 16), ring_lo = desc_lo(smem_u32(smem + L::kRing), 16);
+    const uint32_t v_lo = desc_lo(smem_u32(smem + L::kRing), kBox);
+    Ring<L::kStages> ring;
+    int slot = 0;
+    uint32_t phase = 0, own = 0, half = 0;   // half: one parity bit per (tile, half of P)
+    PkItem it;
+    bool ok = true;
+    while (ok && pk_item(sh, slot, phase, it)) {
+      const int n = max(it.steps[0], it.steps[1]);
+      ok = pk_wait_warp(&sh.own, own, fail);
+      own ^= 1;
+      auto scores = [&](int x, int stage) {   // S of tile x against the K tile in `stage`
+        if (lane == 0) {
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint32_t off = ((ks >> 2) * kBox + (ks & 3) * 32) >> 4;
+            umma_bf16(tmem + x * 128, own_lo + (x * L::kTile >> 4) + off, ring_lo + (stage * L::kTile >> 4) + off, kIdescScores, ks > 0);
+          }
+          umma_commit(&sh.scores[x]);
+        }
+        __syncwarp();
+      };
+      if (ok) ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (it.steps[x] > 0) scores(x, ring.stage);
+      if (lane == 0) {
+        umma_commit(&sh.empty[ring.stage]);
+        if (n == 1) umma_commit(&sh.own_free);
+      }
+      __syncwarp();
+      ring.step();
+      for (int j = 0; j < n && ok; ++j) {
+        const Ring<L::kStages> v = ring;
+        ring.step();                       // now at K(j + 1)
+        ok = pk_wait_warp(&sh.full[v.stage], v.phase, fail);
+        if (!ok) break;
+        // Rows of V behind the sequence belong to others: their probability is 0, but 0 times Inf or NaN is not.
+        const int valid = it.len - j * kPkRows;
+        if (valid < kPkRows) {
+          unsigned char* tile = smem + L::kRing + v.stage * L::kTile;
+          for (int i = valid * 8 + lane; i < kPkRows * 8; i += 32)
+#pragma unroll
+            for (int x = 0; x < L::kBoxes; ++x) *reinterpret_cast<uint4*>(tile + x * kBox + i * 16) = make_uint4(0, 0, 0, 0);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        bool k_here = false;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (j < it.steps[x] && ok) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {   // 64 keys: 4 steps of 16
+              ok = ok && pk_wait_warp(&sh.taken[2 * x + h], (half >> (2 * x + h)) & 1, fail);
+              half ^= 1u << (2 * x + h);
+              if (!ok) break;
+              tc_fence_after();
+              if (lane == 0) {
+#pragma unroll
+                for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
+                  umma_bf16_ta(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, v_lo + (v.stage * L::kTile >> 4) + ks * (2048 >> 4), kIdescOut,
+                               (j > 0 || ks > 0));
+                if (h == 1 && j == it.steps[x] - 1) umma_commit(&sh.done[x]);
+              }
+              __syncwarp();
+            }
+            if (!ok) break;
+          }
+          if (x == 1 && lane == 0) umma_commit(&sh.empty[v.stage]);
+          if (j + 1 < it.steps[x] && ok) {
+            if (!k_here) {
+              ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
+              k_here = true;
+              tc_fence_after();
+            }
+            if (ok) scores(x, ring.stage);
+          }
+        }
+        if (ok && j + 1 < n) {
+          if (lane == 0) {
+            umma_commit(&sh.empty[ring.stage]);
+            if (j + 2 == n) umma_commit(&sh.own_free);
+          }
+          __syncwarp();
+          ring.step();
+        }
+      }
+    }
+    if (!ok || *fail) pk_give_up(sh, p.status);
+  } else {
+    // ===================== softmax: thread <-> query row =====================
+    const int x = warp >> 2, r = tid & 127, w32 = (warp & 3) * 32;
+    const uint32_t lane_addr = (uint32_t)w32 << 16;
+    const uint32_t tS = tmem + x * 128 + lane_addr, tO = tmem + 256 + x * 128 + lane_addr;
+    const float sc = kLog2e * rsqrtf((float)D);
+    int slot = 0;
+    uint32_t phase = 0, s_phase = 0, d_phase = 0;
+    PkItem it;
+    bool ok = true;
+    while (ok && pk_item(sh, slot, phase, it)) {
+      const int n = it.steps[x];
+      if (n == 0) continue;
+      float ref = -INFINITY, l = 0.f;
+      for (int j = 0; j < n; ++j) {
+        ok = pk_wait_warp(&sh.scores[x], s_phase, fail);
+        s_phase ^= 1;
+        if (!ok) break;
+        tc_fence_after();
+        const bool diag = j == n - 1;
+        uint32_t v[2][64];
+        tmem_ld64(tS, v[0]);
+        tmem_ld64(tS + 64, v[1]);
+        if (diag) {   // the tile of this row's own position: keys c > r are not seen
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c > r) v[c >> 6][c & 63] = 0xff800000u;
+        }
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 128; c += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) m4[e] = fmax3(m4[e], __uint_as_float(v[c >> 6][(c & 63) + e]), __uint_as_float(v[c >> 6][(c & 63) + 4 + e]));
+        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
+        float factor = 1.f;
+        if (mx > ref + 32.f || (j == 0 && mx > -INFINITY)) {
+          factor = ref > -INFINITY ? fast_exp2(ref - mx) : 0.f;
+          ref = mx;
+        }
+        l *= factor;
+        if (j > 0 && __any_sync(0xffffffffu, factor != 1.f)) {
+#pragma unroll 1
+          for (int cb = 0; cb < D / 32; ++cb) {
+            uint32_t o[32];
+            tmem_ld32(tO + cb * 32, o);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * factor);
+            tmem_st32(tO + cb * 32, o);
+          }
+        }
+        const float nrf = ref > -INFINITY ? -ref : 0.f;
+        const u64 sc2 = pack2(sc, sc), nrf2 = pack2(nrf, nrf);
+        u64 add[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[32];
+#pragma unroll
+          for (int c = 0; c < 64; c += 2) {
+            u64 t2 = nrf2;
+            fma2(t2, pack2(__uint_as_float(v[h][c]), __uint_as_float(v[h][c + 1])), sc2);
+            float ta, tb;
+            split2(t2, ta, tb);
+            const float pa = fast_exp2(ta), pb = fast_exp2(tb);
+            add[(c >> 1) & 1] = add2(add[(c >> 1) & 1], pack2(pa, pb));
+            w[c >> 1] = bf16_pair(pa, pb);
+          }
+          tmem_st32(tS + h * 32, w);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + h]);
+        }
+        l += sum2(add2(add[0], add[1]));
+      }
+      if (ok) ok = pk_wait_warp(&sh.done[x], d_phase, fail);
+      d_phase ^= 1;
+      if (!ok) break;
+      tc_fence_after();
+      const int qi = it.first[x] + r;
+      const bool live = qi < it.len;
+      const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a sum that is NaN comes through
+      if (live && p.lse) p.lse[(size_t)it.head[x] * p.total + it.row + qi] = ref * kLn2 + logf(l);
+      __nv_bfloat16* orow = static_cast<__nv_bfloat16*>(p.out) + (long long)(it.row + qi) * p.out_token_stride + (long long)it.head[x] * p.out_head_stride;
+#pragma unroll 1
+      for (int cb = 0; cb < D / 32; ++cb) {
+        uint32_t o[32];
+        tmem_ld32(tO + cb * 32, o);
+        if (live) {
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w[e] = bf16_pair(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+          if (p.wide_out) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 8)
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(orow + cb * 32 + 2 * e), "r"(w[e]),
+                           "r"(w[e + 1]), "r"(w[e + 2]), "r"(w[e + 3]), "r"(w[e + 4]), "r"(w[e + 5]), "r"(w[e + 6]), "r"(w[e + 7])
+                           : "memory");
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(orow + cb * 32 + 2 * e) = make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+    }
+    if (!ok) *fail = 1;
+  }
+  pk_end(sh, tmem);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// What each token has received: w_j = sum over heads of the group and queries i >= j of exp2(S_ij - lse_i).
+//   S^T = K Q^T with the keys as rows: a thread owns a key and adds up its row, so nothing is exchanged and no sum's order
+// changes.  Tensor memory holds two S^T for each of the two key tiles; a product runs while the one before it is read.
+// Queries that do not count (before the window, behind the sequence) are left out of the sums.
+// ------------------------------------------------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(kPkThreads, 1)
+st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const PackedParams p) {
+  using L = PkLayout<D>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
+  if (!pk_begin<D>(smem, sh, p.status, 4)) return;
+  const uint32_t tmem = sh.tmem;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int* fail = &sh.fail;
+  const int rows = 2 * kPkRows;
+
+  // Query tiles start at the first query that counts.  steps[x] is the first of them that key tile x takes part in, and
+  // `begin` the number of them in all.
+  if (warp == 9) {
+    Ring<L::kStages> ring;
+    int issued = 0, owned = 0;
+    pk_loader(
+        sh, p.status,
+        [&](int index, PkItem& it) {
+          const int slot = index / p.kv_heads, head = index - slot * p.kv_heads;   // a sequence's first keys, the longest items, first
+          const int b = seq_of(p.cu, p.num_seqs, rows, slot);
+          if (!seq_rows(p, b, it.row, it.len)) return false;
+          if (it.len > p.capacity) {
+            if (p.status && lane == 0) atomicOr(p.status, ST3_DEV_RANGE);
+            return false;
+          }
+          const int rank = slot - (p.cu[b] / rows + b);
+          if (rank < 0 || rank >= (it.len + rows - 1) / rows) return false;
+          it.seq = b;
+          it.begin = p.window > 0 ? max(0, it.len - p.window) : 0;
+          const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            it.head[x] = head;
+            it.first[x] = rank * rows + x * kPkRows;
+            it.steps[x] = it.first[x] < it.len ? max(0, it.first[x] - it.begin) / kPkRows : tiles;
+          }
+          return true;
+        },
+        [&](const PkItem& it) {
+          bool ok = pk_wait_warp(&sh.own_free, (owned & 1) ^ 1, fail);
+          if (!ok) return false;
+          if (lane == 0) {
+            mbar_expect_tx(&sh.own, 2 * L::kTile);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) load_tile<D>(smem + x * L::kTile, &map_k, it.head[x], it.row + it.first[x], &sh.own);
+          }
+          ++owned;
+          const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
+          for (int t = it.steps[0]; t < tiles && ok; ++t)
+            for (int g = 0; g < p.group && ok; ++g) {
+              ok = pk_wait_warp(&sh.empty[ring.stage], ring.phase ^ 1, fail);
+              if (!ok) break;
+              if (lane == 0) {
+                mbar_expect_tx(&sh.full[ring.stage], L::kTile);
+                load_tile<D>(smem + L::kRing + ring.stage * L::kTile, &map_q, it.head[0] * p.group + g, it.row + it.begin + t * kPkRows, &sh.full[ring.stage]);
+              }
+              __syncwarp();
+              ++issued;
+              ring.step();
+            }
+          return ok;
+        });
+    if (lane == 0) pk_settle<L::kStages>(sh, issued, owned);
+    __syncwarp();
+  } else if (warp == 8) {
+    const uint32_t own_lo = desc_lo(smem_u32(smem), 16), ring_lo = desc_lo(smem_u32(smem + L::kRing), 16);
+    Ring<L::kStages> ring;
+    int slot = 0;
+    uint32_t phase = 0, own = 0;
+    uint32_t use[2] = {0, 0};   // S^T buffers used so far, by key tile
+    PkItem it;
+    bool ok = true;
+    while (ok && pk_item(sh, slot, phase, it)) {
+      const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
+      ok = pk_wait_warp(&sh.own, own, fail);
+      own ^= 1;
+      for (int t = it.steps[0]; t < tiles && ok; ++t)
+        for (int g = 0; g < p.group && ok; ++g) {
+          ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
+          if (!ok) break;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (t < it.steps[x] || !ok) continue;
+            const uint32_t buf = use[x] & 1, bar = 2 * x + buf;
+            ok = pk_wait_warp(&sh.taken[bar], ((use[x] >> 1) & 1) ^ 1, fail);
+            if (!ok) break;
+            ++use[x];
+            tc_fence_after();
+            if (lane == 0) {
+#pragma unroll
+              for (int ks = 0; ks < D / 16; ++ks) {
+                const uint32_t off = ((ks >> 2) * kBox + (ks & 3) * 32) >> 4;
+                umma_bf16(tmem + bar * 128, own_lo + (x * L::kTile >> 4) + off, ring_lo + (ring.stage * L::kTile >> 4) + off, kIdescScores, ks > 0);
+              }
+              umma_commit(&sh.scores[bar]);
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
+          if (lane == 0) {
+            umma_commit(&sh.empty[ring.stage]);
+            if (t == tiles - 1 && g == p.group - 1) umma_commit(&sh.own_free);
+          }
+          __syncwarp();
+          ring.step();
+        }
+    }
+    if (!ok || *fail) pk_give_up(sh, p.status);
+  } else {
+    const int x = warp >> 2, r = tid & 127, w32 = (warp & 3) * 32;
+    const uint32_t lane_addr = (uint32_t)w32 << 16;
+    const float sc = kLog2e * rsqrtf((float)D);
+    float* s_lse = reinterpret_cast<float*>(smem + L::kLse) + x * 2 * kPkRows;
+    int slot = 0;
+    uint32_t phase = 0, use = 0;
+    PkItem it;
+    bool ok = true;
+    // the four warps of a tile meet in barriers, so they leave together
+    while (!pk_any_failed(x, !pk_item(sh, slot, phase, it) || !ok)) {
+      const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
+      const int key = it.first[x] + r;
+      u64 acc[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
+      float sum = 0.f;
+      const float* lse = p.lse_in + (size_t)it.head[x] * p.group * p.total + it.row;
+      for (int t = it.steps[x]; t < tiles && ok; ++t) {
+        const int q0 = it.begin + t * kPkRows, valid = min(kPkRows, it.len - q0);
+        const bool edge = q0 < it.first[x] + w32 + 31 || valid < kPkRows;   // some (key, query) of this warp does not count
+        for (int g = 0; g < p.group; ++g) {
+          const uint32_t buf = use & 1;
+          float* s_mine = s_lse + buf * kPkRows;
+          s_mine[r] = r < valid ? -kLog2e * lse[(size_t)g * p.total + q0 + r] : 0.f;
+          if (pk_any_failed(x, !ok)) { ok = false; break; }
+          ok = pk_wait_warp(&sh.scores[2 * x + buf], (use >> 1) & 1, fail);
+          if (!ok) { *fail = 1; continue; }   // told to the others at the next barrier
+          ++use;
+          tc_fence_after();
+          const uint32_t tS = tmem + (2 * x + buf) * 128 + lane_addr;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v[64];
+            tmem_ld64(tS + h * 64, v);
+            if (h == 1) {   // all of S^T is in registers: the next product may overwrite it
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + buf]);
+            }
+            if (!edge) {
+#pragma unroll
+              for (int c = 0; c < 64; c += 4) {
+                const float4 z = *reinterpret_cast<const float4*>(s_mine + h * 64 + c);
+                u64 a = pack2(z.x, z.y), b = pack2(z.z, z.w);
+                const u64 sc2 = pack2(sc, sc);
+                fma2(a, pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2);
+                fma2(b, pack2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2);
+                float a0, a1, b0, b1;
+                split2(a, a0, a1);
+                split2(b, b0, b1);
+                acc[(c >> 1) & 3] = add2(acc[(c >> 1) & 3], pack2(fast_exp2(a0), fast_exp2(a1)));
+                acc[((c >> 1) & 3) + 1] = add2(acc[((c >> 1) & 3) + 1], pack2(fast_exp2(b0), fast_exp2(b1)));
+              }
+            } else {
+              float part = 0.f;
+#pragma unroll
+              for (int c = 0; c < 64; ++c) {
+                const int col = h * 64 + c;
+                const float e = fast_exp2(fmaf(__uint_as_float(v[c]), sc, s_mine[col]));
+                if (col < valid && q0 + col >= key) part += e;
+              }
+              sum += part;
+            }
+          }
+        }
+        // 32-bit sums of at most 128 * group terms each, added up here
+        sum += (sum2(acc[0]) + sum2(acc[1])) + (sum2(acc[2]) + sum2(acc[3]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
+      }
+      if (ok && key < it.len) p.weights[((size_t)it.seq * p.kv_heads + it.head[x]) * p.capacity + key] = sum;
+    }
+    if (!ok) *fail = 1;
+  }
+  pk_end(sh, tmem);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// C ABI
+// ------------------------------------------------------------------------------------------------------------------
+// [total][heads][D] bf16 with any strides, boxes of 128 tokens x 64 elements of one head; tokens outside read as zeros.
+bool packed_map(EncodeTiledFn fn, CUtensorMap* map, const void* base, int dim, int heads, int total, int64_t token_stride, int64_t head_stride) {
+  const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)total};
+  // the stride of a dimension of one is never used, but has to be a valid one
+  const cuuint64_t strides[2] = {(cuuint64_t)(heads > 1 ? head_stride : dim) * 2, (cuuint64_t)(total > 1 ? token_stride : dim) * 2};
+  const cuuint32_t box[3] = {64, 1, kPkRows};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool aligned(const void* p, unsigned a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool strides_ok(int64_t token, int64_t head) {   // what a tensor map takes: positive multiples of 16 bytes below 2^40
+  return token > 0 && head > 0 && token % 8 == 0 && head % 8 == 0 && token < (1ll << 39) && head < (1ll << 39);
+}
+
+st3_status check_packed(const st3_packed* p) {
+  if (!p) return ST3_ERR_INVALID_ARG;
+  if (p->num_seqs < 0 || p->total < 0 || p->num_heads < 1 || p->num_kv_heads < 1 || p->num_heads % p->num_kv_heads) return ST3_ERR_INVALID_ARG;
+  if (p->dtype != ST3_BF16 || (p->head_dim != 64 && p->head_dim != 128)) return ST3_ERR_UNSUPPORTED;
+  if (!strides_ok(p->q_token_stride, p->q_head_stride) || !strides_ok(p->k_token_stride, p->k_head_stride)) return ST3_ERR_INVALID_ARG;
+  // items and tokens are numbered with 31 bits
+  if (((long long)p->total / kPkRows + p->num_seqs) * p->num_heads > 0x7fffffffLL || p->total > 0x7fffff00) return ST3_ERR_UNSUPPORTED;
+  return ST3_OK;
+}
+
+PackedParams packed_params(const st3_packed* p, const int32_t* cu, int* status) {
+  PackedParams d = {};
+  d.cu = cu; d.status = status;
+  d.num_seqs = p->num_seqs; d.total = p->total; d.heads = p->num_heads; d.kv_heads = p->num_kv_heads;
+  d.group = p->num_heads / p->num_kv_heads;
+  return d;
+}
+
+template <int D>
+st3_status attend_launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const PackedParams& d, cudaStream_t s) {
+  if (cudaFuncSetAttribute(st3_packed_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotal) != cudaSuccess) return ST3_ERR_CUDA;
+  return launch(st3_packed_attend_kernel<D>, dim3((unsigned)d.items), dim3(kPkThreads), PkLayout<D>::kTotal, s, mq, mk, mv, d);
+}
+template <int D>
+st3_status weights_launch(const CUtensorMap& mq, const CUtensorMap& mk, const PackedParams& d, cudaStream_t s) {
+  if (cudaFuncSetAttribute(st3_packed_weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotalWeights) != cudaSuccess)
+    return ST3_ERR_CUDA;
+  return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(kPkThreads), PkLayout<D>::kTotalWeights, s, mq, mk, d);
+}
+
+}  // namespace
+
+extern "C" st3_status st3_packed_attend(const st3_packed* p, const void* q, const void* k, const void* v, const int32_t* cu,
+                                        void* out, float* lse, int* dev_status, void* cuda_stream) {
+  const st3_status st = check_packed(p);
+  if (st != ST3_OK) return st;
+  if (!strides_ok(p->v_token_stride, p->v_head_stride) || !strides_ok(p->out_token_stride, p->out_head_stride)) return ST3_ERR_INVALID_ARG;
+  if (!aligned(cu, 4) || (lse && !aligned(lse, 4))) return ST3_ERR_INVALID_ARG;
+  if (p->total == 0 || p->num_seqs == 0) return ST3_OK;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16)) return ST3_ERR_INVALID_ARG;
+  const EncodeTiledFn encode = tensor_map_encoder();
+  CUtensorMap mq, mk, mv;
+  if (!encode || !packed_map(encode, &mq, q, p->head_dim, p->num_heads, p->total, p->q_token_stride, p->q_head_stride) ||
+      !packed_map(encode, &mk, k, p->head_dim, p->num_kv_heads, p->total, p->k_token_stride, p->k_head_stride) ||
+      !packed_map(encode, &mv, v, p->head_dim, p->num_kv_heads, p->total, p->v_token_stride, p->v_head_stride))
+    return ST3_ERR_CUDA;
+  PackedParams d = packed_params(p, cu, dev_status);
+  d.out = out; d.lse = lse;
+  d.out_token_stride = p->out_token_stride; d.out_head_stride = p->out_head_stride;
+  d.wide_out = aligned(out, 32) && p->out_token_stride % 16 == 0 && p->out_head_stride % 16 == 0;
+  d.by_heads = d.group % 2 == 0;
+  d.pairs = d.by_heads ? d.heads / 2 : d.heads;
+  d.items = (d.total / (d.by_heads ? kPkRows : 2 * kPkRows) + d.num_seqs) * d.pairs;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return p->head_dim == 128 ? attend_launch<128>(mq, mk, mv, d, s) : attend_launch<64>(mq, mk, mv, d, s);
+}
+
+extern "C" st3_status st3_packed_weights(const st3_packed* p, const void* q, const void* k, const float* lse, const int32_t* cu,
+                                         float* weights, int32_t capacity, int32_t window, int* dev_status, void* cuda_stream) {
+  const st3_status st = check_packed(p);
+  if (st != ST3_OK) return st;
+  if (capacity < 1 || window < 0 || !aligned(cu, 4) || !aligned(weights, 4) || !aligned(lse, 4)) return ST3_ERR_INVALID_ARG;
+  if (p->total == 0 || p->num_seqs == 0) return ST3_OK;
+  if (!aligned(q, 16) || !aligned(k, 16)) return ST3_ERR_INVALID_ARG;
+  const EncodeTiledFn encode = tensor_map_encoder();
+  CUtensorMap mq, mk;
+  if (!encode || !packed_map(encode, &mq, q, p->head_dim, p->num_heads, p->total, p->q_token_stride, p->q_head_stride) ||
+      !packed_map(encode, &mk, k, p->head_dim, p->num_kv_heads, p->total, p->k_token_stride, p->k_head_stride))
+    return ST3_ERR_CUDA;
+  PackedParams d = packed_params(p, cu, dev_status);
+  d.lse_in = lse; d.weights = weights; d.capacity = capacity; d.window = window;
+  d.pairs = d.kv_heads;
+  d.items = (d.total / (2 * kPkRows) + d.num_seqs) * d.pairs;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return p->head_dim == 128 ? weights_launch<128>(mq, mk, d, s) : weights_launch<64>(mq, mk, d, s);
+}
