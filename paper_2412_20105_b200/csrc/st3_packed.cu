@@ -12,19 +12,23 @@
 // the ceil(n/R) that it needs.  The number of an item says nothing of its sequence's length; numbers without rows are
 // passed over.
 //
-// Roles: warps 0-3 and 4-7 own one tile each, a row (= tensor memory lane) per thread; warp 8 issues the MMAs; warp 9 takes
-// items, decodes them and issues the TMA loads.  Every wait is bounded, and a wait that runs out ends the block's others.
+// Roles: warps 0-3 and 4-7 own one tile each, a row (= tensor memory lane) per thread; warps 8 and 9 issue the MMAs of one tile
+// each; warp 10 takes items, decodes them and issues the TMA loads.  Every wait is bounded, and a wait that runs out ends the block's others.
 #include "st3_common.cuh"
 #include "st3_launch.cuh"
 #include "st3_tensor.cuh"
 
 namespace {
 
-constexpr int kPkThreads = 320;
+constexpr int kPkThreads = 384;              // three warpgroups: one for each tile, and the control warps' (one of them idle)
+constexpr int kPkMma = 8, kPkLoader = 10;    // control warps
+constexpr int kPkRegsRows = 208, kPkRegsControl = 88;   // 2 * 208 + 88 = 3 * 168, the registers of the launch
 constexpr int kPkRows = 128;                 // rows of a tile
 constexpr int kBox = kPkRows * 128;          // one TMA box: 128 rows x 64 bf16
 constexpr uint32_t kPkTmem = 512;
-constexpr uint32_t kIdescScores = kIdescBase | ((128u >> 3) << 17);   // N = 128, both operands K-major
+constexpr int kPkKeys = 64;                  // keys of a step of the attention
+constexpr uint32_t kIdescKeys = kIdescBase | ((kPkKeys >> 3) << 17);   // N = 64, both operands K-major
+constexpr uint32_t kIdescScores = kIdescBase | ((128u >> 3) << 17);    // N = 128
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -58,9 +62,9 @@ struct PkItem {
 struct PkShared {
   uint64_t full[8], empty[8];           // ring of the other operand
   uint64_t own, own_free;               // the item's own two tiles
-  uint64_t scores[4];                   // S is complete (attention: one per tile; weights: two per tile)
-  uint64_t taken[4];                    // attention: P is in tensor memory, by halves; weights: S has been read
-  uint64_t done[2];                     // the last P V of a tile
+  uint64_t scores[4];                   // S is complete (two buffers a tile)
+  uint64_t taken[4];                    // attention: P is in tensor memory; weights: S has been read
+  uint64_t added[2], done[2];           // attention: a P V, and the last one of an item, is complete
   uint64_t ready[2], read[2];           // items
   uint64_t next;                        // answer of the queue
   uint4 answer;
@@ -77,11 +81,10 @@ struct PkLayout {
   static constexpr int kRing = 2 * kTile;
   static constexpr int kShared = kRing + kStages * kTile;
   static constexpr int kLse = kShared + 768;                       // weights: two buffers of 128 sums for each tile
-  static constexpr int kTotal = kShared + 768;
-  static constexpr int kTotalWeights = kLse + 2 * 2 * kPkRows * 4;
+  static constexpr int kTotal = kLse + 2 * 2 * kPkRows * 4;
 };
 static_assert(sizeof(PkShared) <= 768, "PkShared must fit its slot");
-static_assert(PkLayout<128>::kTotalWeights <= 227 * 1024, "shared memory");
+static_assert(PkLayout<128>::kTotal <= 227 * 1024, "shared memory");
 
 // Bounded wait that also ends when another role of the block has given up.
 __device__ __forceinline__ bool pk_wait(uint64_t* bar, uint32_t parity, volatile int* fail) {
@@ -155,24 +158,24 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 
 // The barriers, the tensor memory and the start of a block; false if its shared memory is not where it must be.
 template <int D>
-__device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int* status, int taken_count) {
+__device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int* status) {
   if (smem_u32(smem) & 1023u) {   // the swizzle assumes aligned tiles: reported, not used
     if (threadIdx.x == 0 && status) atomicOr(status, ST3_DEV_RANGE);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     return false;
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < PkLayout<D>::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+    for (int i = 0; i < PkLayout<D>::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 2); }
     mbar_init(&sh.own, 1);
-    mbar_init(&sh.own_free, 1);
-    for (int i = 0; i < 4; ++i) { mbar_init(&sh.scores[i], 1); mbar_init(&sh.taken[i], taken_count); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.done[i], 1); mbar_init(&sh.ready[i], 1); mbar_init(&sh.read[i], 9); }
+    mbar_init(&sh.own_free, 2);
+    for (int i = 0; i < 4; ++i) { mbar_init(&sh.scores[i], 1); mbar_init(&sh.taken[i], 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.added[i], 1); mbar_init(&sh.done[i], 1); mbar_init(&sh.ready[i], 1); mbar_init(&sh.read[i], kPkMma + 2); }
     mbar_init(&sh.next, 1);
     sh.fail = 0;
     mbar_fence_init();
   }
   __syncthreads();
-  if (threadIdx.x >> 5 == 8) {
+  if (threadIdx.x >> 5 == kPkMma) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(kPkTmem) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -186,18 +189,32 @@ __device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int*
 __device__ __forceinline__ void pk_end(PkShared& sh, uint32_t tmem) {
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x >> 5 == 8)
+  if (threadIdx.x >> 5 == kPkMma)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kPkTmem) : "memory");
 }
 
-// Waits for an item and copies it; false when there is none left (or a wait ran out, then `fail` is set).
-__device__ __forceinline__ bool pk_item(PkShared& sh, int& slot, uint32_t& phase, PkItem& it) {
+// Inside the branch of each role: behind a join of the two the compiler would hold everything to the smaller number.
+__device__ __forceinline__ void pk_more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPkRegsRows)); }
+__device__ __forceinline__ void pk_fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPkRegsControl)); }
+
+// Waits for the next item, sh.item[slot]; false when there is none left, or a wait ran out (then `fail` is set).
+__device__ __forceinline__ bool pk_next(PkShared& sh, int slot, uint32_t phase) {
   if (!pk_wait_warp(&sh.ready[slot], phase, &sh.fail)) { *(volatile int*)&sh.fail = 1; return false; }
-  it = sh.item[slot];
+  return !*(volatile int*)&sh.item[slot].stop;
+}
+__device__ __forceinline__ void pk_release(PkShared& sh, int& slot, uint32_t& phase) {
   __syncwarp();
   if ((threadIdx.x & 31) == 0) mbar_arrive_cta(&sh.read[slot]);
   if (++slot == 2) { slot = 0; phase ^= 1; }
-  return !it.stop;
+}
+// The same with a copy of the item.
+__device__ __forceinline__ bool pk_item(PkShared& sh, int& slot, uint32_t& phase, PkItem& it) {
+  const bool more = pk_next(sh, slot, phase);
+  if (more) {
+    it = sh.item[slot];
+    pk_release(sh, slot, phase);
+  }
+  return more;
 }
 
 // The MMA warp's end where a wait has run out: what it has issued (a microsecond's work) ends before tensor memory is given
@@ -210,8 +227,8 @@ __device__ __forceinline__ void pk_give_up(PkShared& sh, int* status) {
   __syncwarp();
 }
 
-// A barrier of the four warps of a tile that tells each of them whether any has failed.
-__device__ __forceinline__ bool pk_any_failed(int tile, bool failed) {
+// A barrier of the four warps of a warpgroup that tells each of them whether any has failed.
+__device__ __forceinline__ bool pk_any_failed(int group, bool failed) {
   uint32_t any;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
@@ -219,7 +236,7 @@ __device__ __forceinline__ bool pk_any_failed(int tile, bool failed) {
       "barrier.cta.red.or.pred q, %2, 128, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(any)
-      : "r"((uint32_t)failed), "r"(1 + tile)
+      : "r"((uint32_t)failed), "r"(1 + group)
       : "memory");
   return any != 0;
 }
@@ -267,6 +284,10 @@ __device__ __forceinline__ void pk_loader(PkShared& sh, int* status, Decode&& de
   __syncwarp();
 }
 
+// The same value in every lane, for the compiler to know.
+template <typename T>
+__device__ __forceinline__ T uniform(T x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // A ring's place: stage and parity of its next use.
 template <int kStages>
 struct Ring {
@@ -287,9 +308,31 @@ __device__ __forceinline__ void pk_settle(PkShared& sh, int issued, int owned) {
 //   S = Q K^T (128 x 128, D/16 MMAs of K = 16), P = exp2(S - ref) as bf16 over the first half of its S, O += P V.
 // The tensor pipe runs PV_A(j) S_A(j+1) | PV_B(j) S_B(j+1) | ...: while one tile's softmax runs, the other tile's two
 // products do.  P goes back in two halves of 64 keys, the first of which P V starts on while the second is computed.  `ref`
-// follows a row's maximum only when that has grown by 2^32: bf16 and fp32 have the range for it and lose no bits, and
+// follows a row's maximum only when that has grown by 2^64: bf16 and fp32 have the range for it and lose no bits, and
 // O is then hardly ever rescaled.  S(j) complete says that P V(j-1) is, which came before it in the pipe.
 // ------------------------------------------------------------------------------------------------------------------
+// exp2(s * sc - ref) of a step's columns, as bf16 pairs in w and added up in `add`.  Whole steps take three pairs of eight on the
+// FMA pipe; where columns are masked (-Inf, which have to give 0) the special-function unit does them all.
+template <bool kWhole>
+__device__ __forceinline__ void probs(const uint32_t (&v)[64], float sc, float ref, u64 (&add)[2], uint32_t (&w)[32]) {
+  const float nrf = ref > -INFINITY ? -ref : 0.f;
+  const u64 sc2 = pack2(sc, sc), nrf2 = pack2(nrf, nrf);
+#pragma unroll
+  for (int c = 0; c < 32; ++c) {
+    const u64 t = mul_add2(pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), sc2, nrf2);
+    float pa, pb;
+    if (kWhole && (c % 8 == 2 || c % 8 == 5 || c % 8 == 7)) {
+      poly_exp2<4>(t, pa, pb);
+    } else {
+      split2(t, pa, pb);
+      pa = fast_exp2(pa);
+      pb = fast_exp2(pb);
+    }
+    add[c & 1] = add2(add[c & 1], pack2(pa, pb));
+    w[c] = bf16_pair(pa, pb);
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPkThreads, 1)
 st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -297,13 +340,15 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
   using L = PkLayout<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
-  if (!pk_begin<D>(smem, sh, p.status, 4)) return;
+  if (!pk_begin<D>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* fail = &sh.fail;
   const int rows = p.by_heads ? kPkRows : 2 * kPkRows;
-
-  if (warp == 9) {
+  if (warp >= kPkMma) pk_fewer_registers();
+  if (warp > kPkLoader) {
+    // idle
+  } else if (warp == kPkLoader) {
     // ===================== loader =====================
     Ring<L::kStages> ring;
     int issued = 0, owned = 0;
@@ -351,182 +396,187 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         });
     if (lane == 0) pk_settle<L::kStages>(sh, issued, owned);
     __syncwarp();
-  } else if (warp == 8) {
-    // ===================== MMA =====================
+  } else if (warp >= kPkMma) {
+    // ===================== MMA: a warp for each tile =====================
     constexpr uint32_t kIdescOut = kIdescBase | (((uint32_t)D >> 3) << 17) | (1u << 16);   // N = D, V MN-major
-    const uint32_t own_lo = desc_lo(smem_u32(smem), 16), ring_lo = desc_lo(smem_u32(smem + L::kRing), 16);
-    const uint32_t v_lo = desc_lo(smem_u32(smem + L::kRing), kBox);
+    const int x = warp - kPkMma;
+    const uint32_t own_lo = uniform(desc_lo(smem_u32(smem + x * L::kTile), 16)), ring_lo = uniform(desc_lo(smem_u32(smem + L::kRing), 16));
+    const uint32_t v_lo = uniform(desc_lo(smem_u32(smem + L::kRing), kBox));
+    const uint32_t tS = uniform(tmem + x * 128), tO = uniform(tmem + 256 + x * 128);
     Ring<L::kStages> ring;
     int slot = 0;
-    uint32_t phase = 0, own = 0, half = 0;   // half: one parity bit per (tile, half of P)
+    uint32_t phase = 0, own = 0, use = 0;   // use: steps so far, two to a tile of keys
     PkItem it;
     bool ok = true;
     while (ok && pk_item(sh, slot, phase, it)) {
-      const int n = max(it.steps[0], it.steps[1]);
+      const int mine = uniform(2 * (x ? it.steps[1] : it.steps[0])), n = uniform(max(it.steps[0], it.steps[1])), len = uniform(it.len);
       ok = pk_wait_warp(&sh.own, own, fail);
       own ^= 1;
-      auto scores = [&](int x, int stage) {   // S of tile x against the K tile in `stage`
-        if (lane == 0) {
+      // S = Q K^T of the two steps of a tile of keys at the ring's place, which is then left
+      Ring<L::kStages> k;
+      auto scores = [&](int t) {
+        if (t < mine) {
+          if (elected()) {
+            const uint32_t k_lo = ring_lo + ((uint32_t)k.stage * L::kTile + (t & 1) * (kPkKeys * 128) >> 4);
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t off = ((ks >> 2) * kBox + (ks & 3) * 32) >> 4;
-            umma_bf16(tmem + x * 128, own_lo + (x * L::kTile >> 4) + off, ring_lo + (stage * L::kTile >> 4) + off, kIdescScores, ks > 0);
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint32_t off = ((ks >> 2) * kBox + (ks & 3) * 32) >> 4;
+              umma_bf16(tS + (t & 1) * kPkKeys, own_lo + off, k_lo + off, kIdescKeys, ks > 0);
+            }
+            umma_commit(&sh.scores[2 * x + (t & 1)]);
           }
-          umma_commit(&sh.scores[x]);
+          __syncwarp();
         }
-        __syncwarp();
+        if (t & 1) {
+          if (elected()) {
+            umma_commit(&sh.empty[k.stage]);
+            if (t == 2 * n - 1) umma_commit(&sh.own_free);
+          }
+          __syncwarp();
+        }
       };
-      if (ok) ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
+      k = ring;
+      ring.step();
+      if (ok) ok = pk_wait_warp(&sh.full[k.stage], k.phase, fail);
       if (!ok) break;
       tc_fence_after();
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        if (it.steps[x] > 0) scores(x, ring.stage);
-      if (lane == 0) {
-        umma_commit(&sh.empty[ring.stage]);
-        if (n == 1) umma_commit(&sh.own_free);
-      }
-      __syncwarp();
-      ring.step();
+      scores(0);
+      scores(1);
       for (int j = 0; j < n && ok; ++j) {
         const Ring<L::kStages> v = ring;
-        ring.step();                       // now at K(j + 1)
+        ring.step();
+        k = ring;                          // K(j + 1)
+        if (j + 1 < n) ring.step();
         ok = pk_wait_warp(&sh.full[v.stage], v.phase, fail);
         if (!ok) break;
-        // Rows of V behind the sequence belong to others: their probability is 0, but 0 times Inf or NaN is not.
-        const int valid = it.len - j * kPkRows;
+        // Rows of V behind the sequence belong to others: their probability is 0, but 0 times Inf or NaN is not.  Both warps
+        // clear them, each before its own product.
+        const int valid = len - j * kPkRows;
         if (valid < kPkRows) {
           unsigned char* tile = smem + L::kRing + v.stage * L::kTile;
           for (int i = valid * 8 + lane; i < kPkRows * 8; i += 32)
 #pragma unroll
-            for (int x = 0; x < L::kBoxes; ++x) *reinterpret_cast<uint4*>(tile + x * kBox + i * 16) = make_uint4(0, 0, 0, 0);
+            for (int y = 0; y < L::kBoxes; ++y) *reinterpret_cast<uint4*>(tile + y * kBox + i * 16) = make_uint4(0, 0, 0, 0);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
-        bool k_here = false;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (j < it.steps[x] && ok) {
+        for (int h = 0; h < 2; ++h) {
+          const int t = 2 * j + h;
+          if (t < mine) {
+            ok = pk_wait_warp(&sh.taken[2 * x + h], (use >> 1) & 1, fail);
+            ++use;
+            if (!ok) break;
+            tc_fence_after();
+            if (elected()) {
+              const uint32_t vb = v_lo + ((uint32_t)v.stage * L::kTile + h * (kPkKeys * 128) >> 4);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {   // 64 keys: 4 steps of 16
-              ok = ok && pk_wait_warp(&sh.taken[2 * x + h], (half >> (2 * x + h)) & 1, fail);
-              half ^= 1u << (2 * x + h);
+              for (int ks = 0; ks < kPkKeys / 16; ++ks)
+                umma_bf16_ta(tO, tS + h * kPkKeys + ks * 8, vb + ks * (2048 >> 4), kIdescOut, (t > 0 || ks > 0));
+              umma_commit(&sh.added[x]);
+              if (t == mine - 1) umma_commit(&sh.done[x]);
+            }
+            __syncwarp();
+          }
+          if (h == 1) {
+            if (elected()) umma_commit(&sh.empty[v.stage]);
+            __syncwarp();
+          }
+          if (j + 1 < n) {
+            if (h == 0) {
+              ok = pk_wait_warp(&sh.full[k.stage], k.phase, fail);
               if (!ok) break;
               tc_fence_after();
-              if (lane == 0) {
-#pragma unroll
-                for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
-                  umma_bf16_ta(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, v_lo + (v.stage * L::kTile >> 4) + ks * (2048 >> 4), kIdescOut,
-                               (j > 0 || ks > 0));
-                if (h == 1 && j == it.steps[x] - 1) umma_commit(&sh.done[x]);
-              }
-              __syncwarp();
             }
-            if (!ok) break;
+            scores(t + 2);
           }
-          if (x == 1 && lane == 0) umma_commit(&sh.empty[v.stage]);
-          if (j + 1 < it.steps[x] && ok) {
-            if (!k_here) {
-              ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
-              k_here = true;
-              tc_fence_after();
-            }
-            if (ok) scores(x, ring.stage);
-          }
-        }
-        if (ok && j + 1 < n) {
-          if (lane == 0) {
-            umma_commit(&sh.empty[ring.stage]);
-            if (j + 2 == n) umma_commit(&sh.own_free);
-          }
-          __syncwarp();
-          ring.step();
         }
       }
     }
     if (!ok || *fail) pk_give_up(sh, p.status);
   } else {
     // ===================== softmax: thread <-> query row =====================
-    const int x = warp >> 2, r = tid & 127, w32 = (warp & 3) * 32;
+    pk_more_registers();
+    const int x = warp >> 2, w32 = (warp & 3) * 32, r = w32 + lane;
     const uint32_t lane_addr = (uint32_t)w32 << 16;
     const uint32_t tS = tmem + x * 128 + lane_addr, tO = tmem + 256 + x * 128 + lane_addr;
     const float sc = kLog2e * rsqrtf((float)D);
     int slot = 0;
-    uint32_t phase = 0, s_phase = 0, d_phase = 0;
-    PkItem it;
+    uint32_t phase = 0, use = 0, d_phase = 0;   // use: steps so far
     bool ok = true;
-    while (ok && pk_item(sh, slot, phase, it)) {
-      const int n = it.steps[x];
-      if (n == 0) continue;
+    while (ok && pk_next(sh, slot, phase)) {
+      const PkItem& it = sh.item[slot];
+      const int n = 2 * it.steps[x];
+      if (n == 0) { pk_release(sh, slot, phase); continue; }
       float ref = -INFINITY, l = 0.f;
-      for (int j = 0; j < n; ++j) {
-        ok = pk_wait_warp(&sh.scores[x], s_phase, fail);
-        s_phase ^= 1;
+      for (int t = 0; t < n; ++t, ++use) {
+        const int h = t & 1;
+        ok = pk_wait_warp(&sh.scores[2 * x + h], (use >> 1) & 1, fail);
         if (!ok) break;
         tc_fence_after();
-        const bool diag = j == n - 1;
-        uint32_t v[2][64];
-        tmem_ld64(tS, v[0]);
-        tmem_ld64(tS + 64, v[1]);
-        if (diag) {   // the tile of this row's own position: keys c > r are not seen
+        const uint32_t tH = tS + h * kPkKeys;
+        const int seen = t >= n - 2 ? r - h * kPkKeys : kPkKeys;   // columns up to this one are seen by this row
+        uint32_t w[32];
+        if (t >= n - 2 && w32 + 31 < h * kPkKeys) {   // none of this warp's rows sees any of them
 #pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if (c > r) v[c >> 6][c & 63] = 0xff800000u;
-        }
-        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (int c = 0; c < 32; ++c) w[c] = 0u;
+        } else {
+          uint32_t v[64];
+          tmem_ld64(tH, v);
+          if (t >= n - 2) {
 #pragma unroll
-        for (int c = 0; c < 128; c += 8)
+            for (int c = 0; c < 64; ++c)
+              if (c > seen) v[c] = 0xff800000u;
+          }
+          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) m4[e] = fmax3(m4[e], __uint_as_float(v[c >> 6][(c & 63) + e]), __uint_as_float(v[c >> 6][(c & 63) + 4 + e]));
-        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
-        float factor = 1.f;
-        if (mx > ref + 32.f || (j == 0 && mx > -INFINITY)) {
-          factor = ref > -INFINITY ? fast_exp2(ref - mx) : 0.f;
-          ref = mx;
-        }
-        l *= factor;
-        if (j > 0 && __any_sync(0xffffffffu, factor != 1.f)) {
+          for (int c = 0; c < 64; c += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m4[e] = fmax3(m4[e], __uint_as_float(v[c + e]), __uint_as_float(v[c + 4 + e]));
+          const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
+          const bool away = mx > ref + 64.f || (ref == -INFINITY && mx > ref);
+          if (__any_sync(0xffffffffu, away)) {
+            const float factor = away ? fast_exp2(ref - mx) : 1.f;   // 0 for the first step
+            if (away) ref = mx;
+            l *= factor;
+            if (t > 0) {
+              // The P V of the step before must be complete.  Waiting for its parity is enough although this thread has not
+              // watched every phase: S is complete, hence the P V issued before it, of two steps ago; and this step's cannot
+              // be issued before the arrival below.
+              ok = pk_wait_warp(&sh.added[x], (use - 1) & 1, fail);
+              if (!ok) break;
+              tc_fence_after();
 #pragma unroll 1
-          for (int cb = 0; cb < D / 32; ++cb) {
-            uint32_t o[32];
-            tmem_ld32(tO + cb * 32, o);
+              for (int cb = 0; cb < D / 32; ++cb) {
+                uint32_t o[32];
+                tmem_ld32(tO + cb * 32, o);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * factor);
-            tmem_st32(tO + cb * 32, o);
+                for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * factor);
+                tmem_st32(tO + cb * 32, o);
+              }
+            }
           }
+          u64 add[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+          if (t < n - 2) probs<true>(v, sc, ref, add, w);
+          else probs<false>(v, sc, ref, add, w);
+          l += sum2(add2(add[0], add[1]));
         }
-        const float nrf = ref > -INFINITY ? -ref : 0.f;
-        const u64 sc2 = pack2(sc, sc), nrf2 = pack2(nrf, nrf);
-        u64 add[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
-#pragma unroll
-          for (int c = 0; c < 64; c += 2) {
-            u64 t2 = nrf2;
-            fma2(t2, pack2(__uint_as_float(v[h][c]), __uint_as_float(v[h][c + 1])), sc2);
-            float ta, tb;
-            split2(t2, ta, tb);
-            const float pa = fast_exp2(ta), pb = fast_exp2(tb);
-            add[(c >> 1) & 1] = add2(add[(c >> 1) & 1], pack2(pa, pb));
-            w[c >> 1] = bf16_pair(pa, pb);
-          }
-          tmem_st32(tS + h * 32, w);
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + h]);
-        }
-        l += sum2(add2(add[0], add[1]));
+        tmem_st32(tH, w);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + h]);
       }
-      if (ok) ok = pk_wait_warp(&sh.done[x], d_phase, fail);
+      if (!ok) break;
+      ok = pk_wait_warp(&sh.done[x], d_phase, fail);
       d_phase ^= 1;
       if (!ok) break;
       tc_fence_after();
-      const int qi = it.first[x] + r;
+      const int qi = it.first[x] + r, head = it.head[x], row = it.row + qi;
       const bool live = qi < it.len;
+      pk_release(sh, slot, phase);
       const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a sum that is NaN comes through
-      if (live && p.lse) p.lse[(size_t)it.head[x] * p.total + it.row + qi] = ref * kLn2 + logf(l);
-      __nv_bfloat16* orow = static_cast<__nv_bfloat16*>(p.out) + (long long)(it.row + qi) * p.out_token_stride + (long long)it.head[x] * p.out_head_stride;
+      if (live && p.lse) p.lse[(size_t)head * p.total + row] = ref * kLn2 + logf(l);
+      __nv_bfloat16* orow = static_cast<__nv_bfloat16*>(p.out) + (long long)row * p.out_token_stride + (long long)head * p.out_head_stride;
 #pragma unroll 1
       for (int cb = 0; cb < D / 32; ++cb) {
         uint32_t o[32];
@@ -567,7 +617,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
   using L = PkLayout<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
-  if (!pk_begin<D>(smem, sh, p.status, 4)) return;
+  if (!pk_begin<D>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* fail = &sh.fail;
@@ -575,7 +625,10 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 
   // Query tiles start at the first query that counts.  steps[x] is the first of them that key tile x takes part in, and
   // `begin` the number of them in all.
-  if (warp == 9) {
+  if (warp >= kPkMma) pk_fewer_registers();
+  if (warp > kPkLoader) {
+    // idle
+  } else if (warp == kPkLoader) {
     Ring<L::kStages> ring;
     int issued = 0, owned = 0;
     pk_loader(
@@ -627,42 +680,40 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         });
     if (lane == 0) pk_settle<L::kStages>(sh, issued, owned);
     __syncwarp();
-  } else if (warp == 8) {
-    const uint32_t own_lo = desc_lo(smem_u32(smem), 16), ring_lo = desc_lo(smem_u32(smem + L::kRing), 16);
+  } else if (warp >= kPkMma) {
+    const int x = warp - kPkMma;   // a warp for each tile
+    const uint32_t own_lo = uniform(desc_lo(smem_u32(smem + x * L::kTile), 16)), ring_lo = uniform(desc_lo(smem_u32(smem + L::kRing), 16));
     Ring<L::kStages> ring;
     int slot = 0;
-    uint32_t phase = 0, own = 0;
-    uint32_t use[2] = {0, 0};   // S^T buffers used so far, by key tile
+    uint32_t phase = 0, own = 0, use = 0;   // use: S^T buffers used so far
     PkItem it;
     bool ok = true;
     while (ok && pk_item(sh, slot, phase, it)) {
-      const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
+      const int tiles = uniform((it.len - it.begin + kPkRows - 1) / kPkRows), mine = uniform(x ? it.steps[1] : it.steps[0]);
       ok = pk_wait_warp(&sh.own, own, fail);
       own ^= 1;
-      for (int t = it.steps[0]; t < tiles && ok; ++t)
+      for (int t = uniform(it.steps[0]); t < tiles && ok; ++t)
         for (int g = 0; g < p.group && ok; ++g) {
           ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
           if (!ok) break;
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            if (t < it.steps[x] || !ok) continue;
-            const uint32_t buf = use[x] & 1, bar = 2 * x + buf;
-            ok = pk_wait_warp(&sh.taken[bar], ((use[x] >> 1) & 1) ^ 1, fail);
+          const bool works = t >= mine;
+          const uint32_t bar = 2 * x + (use & 1);
+          if (works) {
+            ok = pk_wait_warp(&sh.taken[bar], ((use >> 1) & 1) ^ 1, fail);
             if (!ok) break;
-            ++use[x];
-            tc_fence_after();
-            if (lane == 0) {
+            ++use;
+          }
+          tc_fence_after();
+          const uint32_t q_lo = uniform(ring_lo + (uint32_t)ring.stage * (L::kTile >> 4)), tS = uniform(tmem + bar * 128);
+          if (elected()) {
+            if (works) {
 #pragma unroll
               for (int ks = 0; ks < D / 16; ++ks) {
                 const uint32_t off = ((ks >> 2) * kBox + (ks & 3) * 32) >> 4;
-                umma_bf16(tmem + bar * 128, own_lo + (x * L::kTile >> 4) + off, ring_lo + (ring.stage * L::kTile >> 4) + off, kIdescScores, ks > 0);
+                umma_bf16(tS, own_lo + off, q_lo + off, kIdescScores, ks > 0);
               }
               umma_commit(&sh.scores[bar]);
             }
-            __syncwarp();
-          }
-          if (!ok) break;
-          if (lane == 0) {
             umma_commit(&sh.empty[ring.stage]);
             if (t == tiles - 1 && g == p.group - 1) umma_commit(&sh.own_free);
           }
@@ -672,66 +723,66 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     }
     if (!ok || *fail) pk_give_up(sh, p.status);
   } else {
-    const int x = warp >> 2, r = tid & 127, w32 = (warp & 3) * 32;
+    pk_more_registers();
+    const int x = warp >> 2, w32 = (warp & 3) * 32, r = w32 + lane;
     const uint32_t lane_addr = (uint32_t)w32 << 16;
     const float sc = kLog2e * rsqrtf((float)D);
     float* s_lse = reinterpret_cast<float*>(smem + L::kLse) + x * 2 * kPkRows;
     int slot = 0;
     uint32_t phase = 0, use = 0;
-    PkItem it;
     bool ok = true;
     // the four warps of a tile meet in barriers, so they leave together
-    while (!pk_any_failed(x, !pk_item(sh, slot, phase, it) || !ok)) {
-      const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
-      const int key = it.first[x] + r;
+    while (!pk_any_failed(x, !pk_next(sh, slot, phase))) {
+      const PkItem& it = sh.item[slot];
+      const int begin = it.begin, len = it.len, row = it.row, first = it.first[x], t0 = it.steps[x], head = it.head[0], seq = it.seq;
+      pk_release(sh, slot, phase);
+      const int tiles = (len - begin + kPkRows - 1) / kPkRows;
+      const int key = first + r;
       u64 acc[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
       float sum = 0.f;
-      const float* lse = p.lse_in + (size_t)it.head[x] * p.group * p.total + it.row;
-      for (int t = it.steps[x]; t < tiles && ok; ++t) {
-        const int q0 = it.begin + t * kPkRows, valid = min(kPkRows, it.len - q0);
-        const bool edge = q0 < it.first[x] + w32 + 31 || valid < kPkRows;   // some (key, query) of this warp does not count
+      const float* lse = p.lse_in + (size_t)head * p.group * p.total + row;
+      for (int t = t0; t < tiles && ok; ++t) {
+        const int q0 = begin + t * kPkRows, valid = min(kPkRows, len - q0);
+        const bool edge = q0 < first + w32 + 31 || valid < kPkRows;   // some (key, query) of this warp does not count
         for (int g = 0; g < p.group; ++g) {
           const uint32_t buf = use & 1;
-          float* s_mine = s_lse + buf * kPkRows;
-          s_mine[r] = r < valid ? -kLog2e * lse[(size_t)g * p.total + q0 + r] : 0.f;
+          s_lse[buf * kPkRows + r] = r < valid ? -kLog2e * lse[(size_t)g * p.total + q0 + r] : 0.f;
           if (pk_any_failed(x, !ok)) { ok = false; break; }
           ok = pk_wait_warp(&sh.scores[2 * x + buf], (use >> 1) & 1, fail);
           if (!ok) { *fail = 1; continue; }   // told to the others at the next barrier
           ++use;
           tc_fence_after();
-          const uint32_t tS = tmem + (2 * x + buf) * 128 + lane_addr;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             uint32_t v[64];
-            tmem_ld64(tS + h * 64, v);
+            tmem_ld64(tmem + (2 * x + buf) * 128 + h * 64 + lane_addr, v);
             if (h == 1) {   // all of S^T is in registers: the next product may overwrite it
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + buf]);
             }
+            const float* z4 = s_lse + buf * kPkRows + h * 64;
             if (!edge) {
+              const u64 sc2 = pack2(sc, sc);
 #pragma unroll
               for (int c = 0; c < 64; c += 4) {
-                const float4 z = *reinterpret_cast<const float4*>(s_mine + h * 64 + c);
-                u64 a = pack2(z.x, z.y), b = pack2(z.z, z.w);
-                const u64 sc2 = pack2(sc, sc);
-                fma2(a, pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2);
-                fma2(b, pack2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2);
+                const float4 z = *reinterpret_cast<const float4*>(z4 + c);
+                const u64 a = mul_add2(pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, pack2(z.x, z.y));
+                const u64 b = mul_add2(pack2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2, pack2(z.z, z.w));
                 float a0, a1, b0, b1;
                 split2(a, a0, a1);
-                split2(b, b0, b1);
                 acc[(c >> 1) & 3] = add2(acc[(c >> 1) & 3], pack2(fast_exp2(a0), fast_exp2(a1)));
-                acc[((c >> 1) & 3) + 1] = add2(acc[((c >> 1) & 3) + 1], pack2(fast_exp2(b0), fast_exp2(b1)));
+                poly_exp2<5>(b, b0, b1);
+                acc[((c >> 1) & 3) + 1] = add2(acc[((c >> 1) & 3) + 1], pack2(b0, b1));
               }
             } else {
               float part = 0.f;
 #pragma unroll
               for (int c = 0; c < 64; ++c) {
-                const int col = h * 64 + c;
-                const float e = fast_exp2(fmaf(__uint_as_float(v[c]), sc, s_mine[col]));
-                if (col < valid && q0 + col >= key) part += e;
+                const float e = fast_exp2(fmaf(__uint_as_float(v[c]), sc, z4[c]));
+                if (h * 64 + c < valid && q0 + h * 64 + c >= key) part += e;
               }
               sum += part;
             }
@@ -742,7 +793,8 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
       }
-      if (ok && key < it.len) p.weights[((size_t)it.seq * p.kv_heads + it.head[x]) * p.capacity + key] = sum;
+      if (!ok) break;
+      if (key < len) p.weights[((size_t)seq * p.kv_heads + head) * p.capacity + key] = sum;
     }
     if (!ok) *fail = 1;
   }
@@ -793,9 +845,9 @@ st3_status attend_launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUt
 }
 template <int D>
 st3_status weights_launch(const CUtensorMap& mq, const CUtensorMap& mk, const PackedParams& d, cudaStream_t s) {
-  if (cudaFuncSetAttribute(st3_packed_weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotalWeights) != cudaSuccess)
+  if (cudaFuncSetAttribute(st3_packed_weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotal) != cudaSuccess)
     return ST3_ERR_CUDA;
-  return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(kPkThreads), PkLayout<D>::kTotalWeights, s, mq, mk, d);
+  return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(kPkThreads), PkLayout<D>::kTotal, s, mq, mk, d);
 }
 
 }  // namespace

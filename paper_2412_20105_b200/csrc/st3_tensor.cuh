@@ -66,6 +66,13 @@ __device__ __forceinline__ void umma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, u
       : "r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(0u), "r"(kDescHi)
       : "memory");
 }
+// One lane of a whole warp, always the same.  Behind a test of the lane's number the compiler moves every operand of an MMA
+// to the uniform registers anew, and issuing takes longer than the MMA (128x128x16: 115 cycles, 81 behind this).
+__device__ __forceinline__ bool elected() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
 __device__ __forceinline__ void umma_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
                : "memory");
@@ -101,6 +108,14 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t (&r)[64]) {
       : "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n\t"
+      "tcgen05.wait::st.sync.aligned;" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -120,10 +135,44 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+__device__ __forceinline__ u64 mul_add2(u64 a, u64 b, u64 c) {   // a * b + c
+  u64 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
 __device__ __forceinline__ u64 add2(u64 a, u64 b) {
   u64 d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
+}
+// exp2 of a pair on the FMA pipe, for a share of a softmax whose other exponentials keep the special-function unit busy (16 a
+// clock and SM, as many as a D = 128 attention step has in the time of its MMAs).  x = i + f with |f| <= 1/2 by adding and
+// taking away 1.5 * 2^23, whose low bits then hold i; 2^f by a minimax polynomial with p(0) = 1 (least squares, reweighted
+// until the relative error levels: 2.8e-6 at degree 4, 9.2e-8 at degree 5); i goes into the exponent.  Arguments below -126
+// give 2^-126.
+template <int kDegree>
+__device__ __forceinline__ void poly_exp2(u64 x, float& ra, float& rb) {
+  static_assert(kDegree == 4 || kDegree == 5, "coefficients");
+  constexpr float c4[4] = {0.6931241750717163f, 0.24024099111557007f, 0.055906426161527634f, 0.009582852944731712f};
+  constexpr float c5[5] = {0.6931470036506653f, 0.24022242426872253f, 0.05550733581185341f, 0.009671512991189957f, 0.001326472731307149f};
+  float a, b;
+  split2(x, a, b);
+  x = pack2(fmaxf(a, -126.f), fmaxf(b, -126.f));
+  const u64 t = add2(x, pack2(12582912.f, 12582912.f));
+  const u64 f = mul_add2(add2(t, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), x);
+  const float top = kDegree == 4 ? c4[3] : c5[4];
+  u64 p = pack2(top, top);
+#pragma unroll
+  for (int k = kDegree - 2; k >= 0; --k) {
+    const float c = kDegree == 4 ? c4[k < 4 ? k : 3] : c5[k];
+    p = mul_add2(p, f, pack2(c, c));
+  }
+  p = mul_add2(p, f, pack2(1.f, 1.f));
+  float ta, tb;
+  split2(t, ta, tb);
+  split2(p, a, b);
+  ra = __uint_as_float((__float_as_uint(ta) << 23) + __float_as_uint(a));
+  rb = __uint_as_float((__float_as_uint(tb) << 23) + __float_as_uint(b));
 }
 // kind::f16 instruction descriptor without N: fp32 accumulate, bf16 x bf16, M = 128.
 constexpr uint32_t kIdescBase = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);
