@@ -12,17 +12,25 @@
 // the ceil(n/R) that it needs.  The number of an item says nothing of its sequence's length; numbers without rows are
 // passed over.
 //
-// Roles: warps 0-3 and 4-7 own one tile each, a row (= tensor memory lane) per thread; warps 8 and 9 issue the MMAs of one tile
-// each; warp 10 takes items, decodes them and issues the TMA loads.  Every wait is bounded, and a wait that runs out ends the block's others.
+// Roles: four warps (attention) or eight (weights) own a tile each, a row (= tensor memory lane) per thread, in the weights
+// with half of the columns; two warps issue the MMAs of one tile each; one takes items, decodes them and issues the TMA loads.
+// Every wait is bounded, and a wait that runs out ends the block's others.
 #include "st3_common.cuh"
 #include "st3_launch.cuh"
 #include "st3_tensor.cuh"
 
 namespace {
 
-constexpr int kPkThreads = 384;              // three warpgroups: one for each tile, and the control warps' (one of them idle)
-constexpr int kPkMma = 8, kPkLoader = 10;    // control warps
-constexpr int kPkRegsRows = 208, kPkRegsControl = 88;   // 2 * 208 + 88 = 3 * 168, the registers of the launch
+// A block of kWarps warps that own rows and a warpgroup of control warps (one of them idle).  The registers of the launch are
+// shared out anew: what the owners of rows get and the control warps keep adds up to them.
+template <int kWarps>
+struct PkRoles {
+  static constexpr int kMma = kWarps, kLoader = kWarps + 2, kThreads = (kWarps + 4) * 32;
+  static constexpr int kRegsRows = kWarps == 8 ? 208 : 104, kRegsControl = kWarps == 8 ? 88 : 64;
+  static_assert(kWarps == 8 || kWarps == 16, "2 * 208 + 88 = 3 * 168; 4 * 104 + 64 = 5 * 96");
+};
+using AttendRoles = PkRoles<8>;
+using WeightRoles = PkRoles<16>;
 constexpr int kPkRows = 128;                 // rows of a tile
 constexpr int kBox = kPkRows * 128;          // one TMA box: 128 rows x 64 bf16
 constexpr uint32_t kPkTmem = 512;
@@ -80,11 +88,11 @@ struct PkLayout {
   static constexpr int kStages = D == 128 ? 5 : 8;
   static constexpr int kRing = 2 * kTile;
   static constexpr int kShared = kRing + kStages * kTile;
-  static constexpr int kLse = kShared + 768;                       // weights: two buffers of 128 sums for each tile
-  static constexpr int kTotal = kLse + 2 * 2 * kPkRows * 4;
+  static constexpr int kLse = kShared + 768;                       // weights: two buffers of 64 sums for each warpgroup
+  static constexpr int kTotal = kShared + 768, kTotalWeights = kLse + 4 * 2 * 64 * 4;
 };
 static_assert(sizeof(PkShared) <= 768, "PkShared must fit its slot");
-static_assert(PkLayout<128>::kTotal <= 227 * 1024, "shared memory");
+static_assert(PkLayout<128>::kTotalWeights <= 227 * 1024, "shared memory");
 
 // Bounded wait that also ends when another role of the block has given up.
 __device__ __forceinline__ bool pk_wait(uint64_t* bar, uint32_t parity, volatile int* fail) {
@@ -157,7 +165,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 }
 
 // The barriers, the tensor memory and the start of a block; false if its shared memory is not where it must be.
-template <int D>
+template <int D, typename Roles>
 __device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int* status) {
   if (smem_u32(smem) & 1023u) {   // the swizzle assumes aligned tiles: reported, not used
     if (threadIdx.x == 0 && status) atomicOr(status, ST3_DEV_RANGE);
@@ -168,14 +176,14 @@ __device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int*
     for (int i = 0; i < PkLayout<D>::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 2); }
     mbar_init(&sh.own, 1);
     mbar_init(&sh.own_free, 2);
-    for (int i = 0; i < 4; ++i) { mbar_init(&sh.scores[i], 1); mbar_init(&sh.taken[i], 4); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.added[i], 1); mbar_init(&sh.done[i], 1); mbar_init(&sh.ready[i], 1); mbar_init(&sh.read[i], kPkMma + 2); }
+    for (int i = 0; i < 4; ++i) { mbar_init(&sh.scores[i], 1); mbar_init(&sh.taken[i], Roles::kMma / 2); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.added[i], 1); mbar_init(&sh.done[i], 1); mbar_init(&sh.ready[i], 1); mbar_init(&sh.read[i], Roles::kMma + 2); }
     mbar_init(&sh.next, 1);
     sh.fail = 0;
     mbar_fence_init();
   }
   __syncthreads();
-  if (threadIdx.x >> 5 == kPkMma) {
+  if (threadIdx.x >> 5 == Roles::kMma) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(kPkTmem) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -186,16 +194,19 @@ __device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int*
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   return true;
 }
+template <typename Roles>
 __device__ __forceinline__ void pk_end(PkShared& sh, uint32_t tmem) {
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x >> 5 == kPkMma)
+  if (threadIdx.x >> 5 == Roles::kMma)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kPkTmem) : "memory");
 }
 
 // Inside the branch of each role: behind a join of the two the compiler would hold everything to the smaller number.
-__device__ __forceinline__ void pk_more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPkRegsRows)); }
-__device__ __forceinline__ void pk_fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPkRegsControl)); }
+template <typename Roles>
+__device__ __forceinline__ void pk_more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Roles::kRegsRows)); }
+template <typename Roles>
+__device__ __forceinline__ void pk_fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Roles::kRegsControl)); }
 
 // Waits for the next item, sh.item[slot]; false when there is none left, or a wait ran out (then `fail` is set).
 __device__ __forceinline__ bool pk_next(PkShared& sh, int slot, uint32_t phase) {
@@ -227,16 +238,16 @@ __device__ __forceinline__ void pk_give_up(PkShared& sh, int* status) {
   __syncwarp();
 }
 
-// A barrier of the four warps of a warpgroup that tells each of them whether any has failed.
-__device__ __forceinline__ bool pk_any_failed(int group, bool failed) {
+// A barrier of the eight warps of a tile of the weights that tells each of them whether any has failed.
+__device__ __forceinline__ bool pk_any_failed(int tile, bool failed) {
   uint32_t any;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, %2, 128, p;\n\t"
+      "barrier.cta.red.or.pred q, %2, 256, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(any)
-      : "r"((uint32_t)failed), "r"(1 + group)
+      : "r"((uint32_t)failed), "r"(1 + tile)
       : "memory");
   return any != 0;
 }
@@ -311,7 +322,7 @@ __device__ __forceinline__ void pk_settle(PkShared& sh, int issued, int owned) {
 // follows a row's maximum only when that has grown by 2^64: bf16 and fp32 have the range for it and lose no bits, and
 // O is then hardly ever rescaled.  S(j) complete says that P V(j-1) is, which came before it in the pipe.
 // ------------------------------------------------------------------------------------------------------------------
-// exp2(s * sc - ref) of a step's columns, as bf16 pairs in w and added up in `add`.  Whole steps take three pairs of eight on the
+// exp2(s * sc - ref) of a step's columns, as bf16 pairs in w and added up in `add`.  Whole steps take every fourth pair on the
 // FMA pipe; where columns are masked (-Inf, which have to give 0) the special-function unit does them all.
 template <bool kWhole>
 __device__ __forceinline__ void probs(const uint32_t (&v)[64], float sc, float ref, u64 (&add)[2], uint32_t (&w)[32]) {
@@ -321,7 +332,7 @@ __device__ __forceinline__ void probs(const uint32_t (&v)[64], float sc, float r
   for (int c = 0; c < 32; ++c) {
     const u64 t = mul_add2(pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), sc2, nrf2);
     float pa, pb;
-    if (kWhole && (c % 8 == 2 || c % 8 == 5 || c % 8 == 7)) {
+    if (kWhole && c % 4 == 2) {
       poly_exp2<4>(t, pa, pb);
     } else {
       split2(t, pa, pb);
@@ -334,21 +345,21 @@ __device__ __forceinline__ void probs(const uint32_t (&v)[64], float sc, float r
 }
 
 template <int D>
-__global__ void __launch_bounds__(kPkThreads, 1)
+__global__ void __launch_bounds__(AttendRoles::kThreads, 1)
 st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                          const __grid_constant__ CUtensorMap map_v, const PackedParams p) {
   using L = PkLayout<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
-  if (!pk_begin<D>(smem, sh, p.status)) return;
+  if (!pk_begin<D, AttendRoles>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* fail = &sh.fail;
   const int rows = p.by_heads ? kPkRows : 2 * kPkRows;
-  if (warp >= kPkMma) pk_fewer_registers();
-  if (warp > kPkLoader) {
+  if (warp >= AttendRoles::kMma) pk_fewer_registers<AttendRoles>();
+  if (warp > AttendRoles::kLoader) {
     // idle
-  } else if (warp == kPkLoader) {
+  } else if (warp == AttendRoles::kLoader) {
     // ===================== loader =====================
     Ring<L::kStages> ring;
     int issued = 0, owned = 0;
@@ -396,10 +407,10 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         });
     if (lane == 0) pk_settle<L::kStages>(sh, issued, owned);
     __syncwarp();
-  } else if (warp >= kPkMma) {
+  } else if (warp >= AttendRoles::kMma) {
     // ===================== MMA: a warp for each tile =====================
     constexpr uint32_t kIdescOut = kIdescBase | (((uint32_t)D >> 3) << 17) | (1u << 16);   // N = D, V MN-major
-    const int x = warp - kPkMma;
+    const int x = warp - AttendRoles::kMma;
     const uint32_t own_lo = uniform(desc_lo(smem_u32(smem + x * L::kTile), 16)), ring_lo = uniform(desc_lo(smem_u32(smem + L::kRing), 16));
     const uint32_t v_lo = uniform(desc_lo(smem_u32(smem + L::kRing), kBox));
     const uint32_t tS = uniform(tmem + x * 128), tO = uniform(tmem + 256 + x * 128);
@@ -496,7 +507,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     if (!ok || *fail) pk_give_up(sh, p.status);
   } else {
     // ===================== softmax: thread <-> query row =====================
-    pk_more_registers();
+    pk_more_registers<AttendRoles>();
     const int x = warp >> 2, w32 = (warp & 3) * 32, r = w32 + lane;
     const uint32_t lane_addr = (uint32_t)w32 << 16;
     const uint32_t tS = tmem + x * 128 + lane_addr, tO = tmem + 256 + x * 128 + lane_addr;
@@ -602,7 +613,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     }
     if (!ok) *fail = 1;
   }
-  pk_end(sh, tmem);
+  pk_end<AttendRoles>(sh, tmem);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -611,13 +622,43 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 // changes.  Tensor memory holds two S^T for each of the two key tiles; a product runs while the one before it is read.
 // Queries that do not count (before the window, behind the sequence) are left out of the sums.
 // ------------------------------------------------------------------------------------------------------------------
+// Adds exp2(s * sc - lse) of 32 queries; kSome: of those in [lo, hi) only, whatever the others are.
+template <bool kSome>
+__device__ __forceinline__ void add_weights(const uint32_t (&v)[64], int part, const float* s_lse, float sc, int lo, int hi, u64 (&acc)[4]) {
+  const u64 sc2 = pack2(sc, sc);
+#pragma unroll
+  for (int c = 0; c < 32; c += 4) {
+    const float4 z = *reinterpret_cast<const float4*>(s_lse + c);
+    const int at = part * 32 + c;
+    const u64 a = mul_add2(pack2(__uint_as_float(v[at]), __uint_as_float(v[at + 1])), sc2, pack2(z.x, z.y));
+    const u64 b = mul_add2(pack2(__uint_as_float(v[at + 2]), __uint_as_float(v[at + 3])), sc2, pack2(z.z, z.w));
+    float e[4];
+    split2(a, e[0], e[1]);
+    e[0] = fast_exp2(e[0]);
+    e[1] = fast_exp2(e[1]);
+    if (c & 4) {   // a quarter of the exponentials on the FMA pipe
+      poly_exp2<5>(b, e[2], e[3]);
+    } else {
+      split2(b, e[2], e[3]);
+      e[2] = fast_exp2(e[2]);
+      e[3] = fast_exp2(e[3]);
+    }
+    if (kSome) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i] = c + i >= lo && c + i < hi ? e[i] : 0.f;
+    }
+    acc[(c >> 1) & 3] = add2(acc[(c >> 1) & 3], pack2(e[0], e[1]));
+    acc[((c >> 1) & 3) + 1] = add2(acc[((c >> 1) & 3) + 1], pack2(e[2], e[3]));
+  }
+}
+
 template <int D>
-__global__ void __launch_bounds__(kPkThreads, 1)
+__global__ void __launch_bounds__(WeightRoles::kThreads, 1)
 st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const PackedParams p) {
   using L = PkLayout<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
-  if (!pk_begin<D>(smem, sh, p.status)) return;
+  if (!pk_begin<D, WeightRoles>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* fail = &sh.fail;
@@ -625,10 +666,10 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 
   // Query tiles start at the first query that counts.  steps[x] is the first of them that key tile x takes part in, and
   // `begin` the number of them in all.
-  if (warp >= kPkMma) pk_fewer_registers();
-  if (warp > kPkLoader) {
+  if (warp >= WeightRoles::kMma) pk_fewer_registers<WeightRoles>();
+  if (warp > WeightRoles::kLoader) {
     // idle
-  } else if (warp == kPkLoader) {
+  } else if (warp == WeightRoles::kLoader) {
     Ring<L::kStages> ring;
     int issued = 0, owned = 0;
     pk_loader(
@@ -680,8 +721,8 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         });
     if (lane == 0) pk_settle<L::kStages>(sh, issued, owned);
     __syncwarp();
-  } else if (warp >= kPkMma) {
-    const int x = warp - kPkMma;   // a warp for each tile
+  } else if (warp >= WeightRoles::kMma) {
+    const int x = warp - WeightRoles::kMma;   // a warp for each tile
     const uint32_t own_lo = uniform(desc_lo(smem_u32(smem + x * L::kTile), 16)), ring_lo = uniform(desc_lo(smem_u32(smem + L::kRing), 16));
     Ring<L::kStages> ring;
     int slot = 0;
@@ -723,82 +764,77 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     }
     if (!ok || *fail) pk_give_up(sh, p.status);
   } else {
-    pk_more_registers();
-    const int x = warp >> 2, w32 = (warp & 3) * 32, r = w32 + lane;
+    pk_more_registers<WeightRoles>();
+    const int group = warp >> 2, x = group >> 1, half = group & 1, w32 = (warp & 3) * 32, r = w32 + lane;
     const uint32_t lane_addr = (uint32_t)w32 << 16;
     const float sc = kLog2e * rsqrtf((float)D);
-    float* s_lse = reinterpret_cast<float*>(smem + L::kLse) + x * 2 * kPkRows;
+    float* s_rows = reinterpret_cast<float*>(smem + L::kLse);
+    float* s_lse = s_rows + group * 128;   // two buffers of this warpgroup's 64 queries
     int slot = 0;
     uint32_t phase = 0, use = 0;
     bool ok = true;
-    // the four warps of a tile meet in barriers, so they leave together
+    // the warps of a tile meet in barriers, so they leave together
     while (!pk_any_failed(x, !pk_next(sh, slot, phase))) {
       const PkItem& it = sh.item[slot];
-      const int begin = it.begin, len = it.len, row = it.row, first = it.first[x], t0 = it.steps[x], head = it.head[0], seq = it.seq;
-      pk_release(sh, slot, phase);
+      const int begin = it.begin, len = it.len, first = it.first[x], t0 = it.steps[x];
       const int tiles = (len - begin + kPkRows - 1) / kPkRows;
       const int key = first + r;
       u64 acc[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
       float sum = 0.f;
-      const float* lse = p.lse_in + (size_t)head * p.group * p.total + row;
+      bool left = false;   // the verdict that ends the loops has been given
+      // one step ahead: the load's latency runs under the step before, so nothing may be made of it before then
+      const float* lse = p.lse_in + (size_t)it.head[0] * p.group * p.total + it.row;
+      auto load_lse = [&](int t, int g) {
+        const int q = begin + t * kPkRows + half * 64 + r;
+        return r < 64 && t < tiles && q < len ? lse[(size_t)g * p.total + q] : 0.f;
+      };
+      float next = load_lse(t0, 0);
       for (int t = t0; t < tiles && ok; ++t) {
-        const int q0 = begin + t * kPkRows, valid = min(kPkRows, len - q0);
-        const bool edge = q0 < first + w32 + 31 || valid < kPkRows;   // some (key, query) of this warp does not count
+        const int q0 = begin + t * kPkRows + half * 64, valid = len - q0;
         for (int g = 0; g < p.group; ++g) {
           const uint32_t buf = use & 1;
-          s_lse[buf * kPkRows + r] = r < valid ? -kLog2e * lse[(size_t)g * p.total + q0 + r] : 0.f;
-          if (pk_any_failed(x, !ok)) { ok = false; break; }
+          if (r < 64) s_lse[buf * 64 + r] = -kLog2e * next;
+          if (pk_any_failed(x, !ok)) { ok = false; left = true; break; }
+          next = g + 1 < p.group ? load_lse(t, g + 1) : load_lse(t + 1, 0);
           ok = pk_wait_warp(&sh.scores[2 * x + buf], (use >> 1) & 1, fail);
           if (!ok) { *fail = 1; continue; }   // told to the others at the next barrier
           ++use;
           tc_fence_after();
+          uint32_t v[64];
+          tmem_ld64(tmem + (2 * x + buf) * 128 + half * 64 + lane_addr, v);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + buf]);   // the next product may overwrite it
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t v[64];
-            tmem_ld64(tmem + (2 * x + buf) * 128 + h * 64 + lane_addr, v);
-            if (h == 1) {   // all of S^T is in registers: the next product may overwrite it
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + buf]);
-            }
-            const float* z4 = s_lse + buf * kPkRows + h * 64;
-            if (!edge) {
-              const u64 sc2 = pack2(sc, sc);
-#pragma unroll
-              for (int c = 0; c < 64; c += 4) {
-                const float4 z = *reinterpret_cast<const float4*>(z4 + c);
-                const u64 a = mul_add2(pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, pack2(z.x, z.y));
-                const u64 b = mul_add2(pack2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2, pack2(z.z, z.w));
-                float a0, a1, b0, b1;
-                split2(a, a0, a1);
-                acc[(c >> 1) & 3] = add2(acc[(c >> 1) & 3], pack2(fast_exp2(a0), fast_exp2(a1)));
-                poly_exp2<5>(b, b0, b1);
-                acc[((c >> 1) & 3) + 1] = add2(acc[((c >> 1) & 3) + 1], pack2(b0, b1));
-              }
-            } else {
-              float part = 0.f;
-#pragma unroll
-              for (int c = 0; c < 64; ++c) {
-                const float e = fast_exp2(fmaf(__uint_as_float(v[c]), sc, z4[c]));
-                if (h * 64 + c < valid && q0 + h * 64 + c >= key) part += e;
-              }
-              sum += part;
-            }
+          for (int part = 0; part < 2; ++part) {   // 32 queries, of which none, all or some count for this warp's keys
+            const int c0 = part * 32, lo = key - q0 - c0, hi = valid - c0;
+            const int warp_lo = first + w32 - q0 - c0;   // the warp's first key; its last is 31 further
+            if (warp_lo > 31 || hi <= 0) continue;
+            if (warp_lo + 31 <= 0 && hi >= 32) add_weights<false>(v, part, s_lse + buf * 64 + c0, sc, 0, 32, acc);
+            else add_weights<true>(v, part, s_lse + buf * 64 + c0, sc, lo, hi, acc);
           }
         }
-        // 32-bit sums of at most 128 * group terms each, added up here
+        // 32-bit sums of at most 64 * group terms each, added up here
         sum += (sum2(acc[0]) + sum2(acc[1])) + (sum2(acc[2]) + sum2(acc[3]));
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
       }
-      if (!ok) break;
-      if (key < len) p.weights[((size_t)seq * p.kv_heads + head) * p.capacity + key] = sum;
+      const int seq = it.seq, head = it.head[0];
+      pk_release(sh, slot, phase);
+      // the second half's sums go to the first half's threads, through the places of the second half's lse
+      const int pair_bar = 3 + x * 4 + (warp & 3);
+      float* s_sum = s_rows + (2 * x + 1) * 128 + r;
+      if (left || pk_any_failed(x, !ok)) { ok = false; break; }   // all of them have read their lse
+      if (half == 1) *s_sum = sum;
+      asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+      if (half == 0 && key < len) p.weights[((size_t)seq * p.kv_heads + head) * p.capacity + key] = sum + *s_sum;
+      asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
     }
     if (!ok) *fail = 1;
   }
-  pk_end(sh, tmem);
+  pk_end<WeightRoles>(sh, tmem);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -841,13 +877,13 @@ PackedParams packed_params(const st3_packed* p, const int32_t* cu, int* status) 
 template <int D>
 st3_status attend_launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const PackedParams& d, cudaStream_t s) {
   if (cudaFuncSetAttribute(st3_packed_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotal) != cudaSuccess) return ST3_ERR_CUDA;
-  return launch(st3_packed_attend_kernel<D>, dim3((unsigned)d.items), dim3(kPkThreads), PkLayout<D>::kTotal, s, mq, mk, mv, d);
+  return launch(st3_packed_attend_kernel<D>, dim3((unsigned)d.items), dim3(AttendRoles::kThreads), PkLayout<D>::kTotal, s, mq, mk, mv, d);
 }
 template <int D>
 st3_status weights_launch(const CUtensorMap& mq, const CUtensorMap& mk, const PackedParams& d, cudaStream_t s) {
-  if (cudaFuncSetAttribute(st3_packed_weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotal) != cudaSuccess)
+  if (cudaFuncSetAttribute(st3_packed_weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotalWeights) != cudaSuccess)
     return ST3_ERR_CUDA;
-  return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(kPkThreads), PkLayout<D>::kTotal, s, mq, mk, d);
+  return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(WeightRoles::kThreads), PkLayout<D>::kTotalWeights, s, mq, mk, d);
 }
 
 }  // namespace
