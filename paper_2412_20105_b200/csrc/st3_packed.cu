@@ -260,11 +260,7 @@ __device__ __forceinline__ void pk_loader(PkShared& sh, int* status, Decode&& de
   int index = blockIdx.x, slot = 0;
   uint32_t phase = 1, answer = 0;
   bool ok = true;
-  while (ok) {
-    if (lane == 0) {
-      mbar_expect_tx(&sh.next, 16);
-      take_next(&sh.answer, &sh.next);
-    }
+  while (true) {
     PkItem it;
     if (decode(index, it)) {
       ok = pk_wait_warp(&sh.read[slot], phase, &sh.fail);
@@ -274,6 +270,13 @@ __device__ __forceinline__ void pk_loader(PkShared& sh, int* status, Decode&& de
         if (++slot == 2) { slot = 0; phase ^= 1; }
         ok = load(it);
       }
+      if (!ok) break;
+    }
+    // The next item is taken when this one's last tiles have been requested, which is a few steps ahead of their use: taken any
+    // earlier, it would stay with this block while others run out of work (weights of 16 x 690 tokens: 98 -> 85 us).
+    if (lane == 0) {
+      mbar_expect_tx(&sh.next, 16);
+      take_next(&sh.answer, &sh.next);
     }
     // the answer is waited for also where the block gives up: it is written into this block's shared memory
     if (!pk_wait_warp(&sh.next, answer, &sh.fail) && !pf_wait_warp(&sh.next, answer)) { ok = false; break; }
