@@ -312,30 +312,31 @@ def _dtype_of(t) -> int:
     return _DTYPES[t.dtype]
 
 
-def _stream_of(t) -> int:
-    """The current stream of the tensor's device, which has to be the current device."""
+def _stream_of(index: int) -> int:
+    """The current stream of that device, which has to be the current one."""
     import torch
-    index = t.device.index
-    if not t.is_cuda or index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if index != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on cuda:{index}, the current device is cuda:{torch._C._cuda_getDevice()}")
     return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _dense(t, shape, dtype, device, what):
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous {dtype} tensor of {tuple(shape)} on {device} is needed, "
-                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
+def _dense(t, shape, dtype, index, what):
+    """Address of a dense tensor on CUDA device `index`."""
+    if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.is_cuda and t.get_device() == index:
+        return t.data_ptr()
+    raise ValueError(f"{what}: a contiguous {dtype} tensor of {tuple(shape)} on cuda:{index} is needed, "
+                     f"not {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _rows_view(t, heads, dim, dtype, device, what):
+def _rows_view(t, heads, dim, dtype, index, what):
     """Address and (token, head) strides of a [tokens, heads, dim] tensor whose last dimension is dense."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{what}: a {dtype} tensor of [tokens, {heads}, {dim}] on {device} is needed, "
+    if t.dim() != 3 or t.size(1) != heads or t.size(2) != dim or t.dtype is not dtype or not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{what}: a {dtype} tensor of [tokens, {heads}, {dim}] on cuda:{index} is needed, "
                          f"not {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.stride(2) != 1:
+    token, head, one = t.stride()
+    if one != 1:
         raise ValueError(f"{what}: the elements of a head have to lie side by side")
-    return t.data_ptr(), (t.stride(0), t.stride(1))
+    return t.data_ptr(), (token, head)
 
 
 def _packed(q, k, cu):
@@ -343,27 +344,27 @@ def _packed(q, k, cu):
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k: tensors of [tokens, heads, dim] are needed")
     total, heads, dim = q.shape
-    qp, qs = _rows_view(q, heads, dim, q.dtype, q.device, "q")
-    kp, ks = _rows_view(k, k.shape[1], dim, q.dtype, q.device, "k")
+    qp, qs = _rows_view(q, heads, dim, q.dtype, q.get_device(), "q")
+    kp, ks = _rows_view(k, k.shape[1], dim, q.dtype, q.get_device(), "k")
     if k.shape[0] != total:
         raise ValueError("q and k have different numbers of tokens")
     if cu.dim() != 1 or cu.numel() < 1:
         raise ValueError("cu: [sequences + 1] is needed")
     desc = PackedDesc(cu.numel() - 1, total, heads, k.shape[1], dim, _dtype_of(q), *qs, *ks, *ks, *qs)
-    return desc, qp, kp, _dense(cu, cu.shape, torch.int32, q.device, "cu")
+    return desc, qp, kp, _dense(cu, cu.shape, torch.int32, q.get_device(), "cu")
 
 
 def packed_attend(q, k, v, cu, out, lse=None, status=None):
     """Causal attention of packed prompts: q, out [tokens, heads, dim], k, v [tokens, kv heads, dim], lse [heads, tokens]."""
     import torch
     desc, qp, kp, cup = _packed(q, k, cu)
-    vp, (desc.v_token_stride, desc.v_head_stride) = _rows_view(v, k.shape[1], q.shape[2], q.dtype, q.device, "v")
-    op, (desc.out_token_stride, desc.out_head_stride) = _rows_view(out, q.shape[1], q.shape[2], q.dtype, q.device, "out")
+    vp, (desc.v_token_stride, desc.v_head_stride) = _rows_view(v, k.shape[1], q.shape[2], q.dtype, q.get_device(), "v")
+    op, (desc.out_token_stride, desc.out_head_stride) = _rows_view(out, q.shape[1], q.shape[2], q.dtype, q.get_device(), "out")
     if v.shape[0] != q.shape[0] or out.shape[0] != q.shape[0]:
         raise ValueError("q, v and out have different numbers of tokens")
     st3_packed_attend(desc, qp, kp, vp, cup, op,
-                      None if lse is None else _dense(lse, (q.shape[1], q.shape[0]), torch.float32, q.device, "lse"),
-                      None if status is None else _dense(status, (1,), torch.int32, q.device, "status"), _stream_of(q))
+                      None if lse is None else _dense(lse, (q.shape[1], q.shape[0]), torch.float32, q.get_device(), "lse"),
+                      None if status is None else _dense(status, (1,), torch.int32, q.get_device(), "status"), _stream_of(q.get_device()))
 
 
 def packed_weights(q, k, lse, cu, weights, window=0, status=None):
@@ -373,9 +374,9 @@ def packed_weights(q, k, lse, cu, weights, window=0, status=None):
     if weights.dim() != 3:
         raise ValueError("weights: [sequences, kv heads, capacity] is needed")
     shape = (desc.num_seqs, desc.num_kv_heads, weights.shape[2])
-    st3_packed_weights(desc, qp, kp, _dense(lse, (q.shape[1], q.shape[0]), torch.float32, q.device, "lse"), cup,
-                       _dense(weights, shape, torch.float32, q.device, "weights"), weights.shape[2], window,
-                       None if status is None else _dense(status, (1,), torch.int32, q.device, "status"), _stream_of(q))
+    st3_packed_weights(desc, qp, kp, _dense(lse, (q.shape[1], q.shape[0]), torch.float32, q.get_device(), "lse"), cup,
+                       _dense(weights, shape, torch.float32, q.get_device(), "weights"), weights.shape[2], window,
+                       None if status is None else _dense(status, (1,), torch.int32, q.get_device(), "status"), _stream_of(q.get_device()))
 
 
 class Cache:
@@ -392,13 +393,14 @@ class Cache:
         if not k.is_cuda:
             raise ValueError("a CUDA device is required: this library has no CPU path")
         self.torch, self.device = torch, k.device
+        index = self._index = k.get_device()
         self.k, self.v, self.k_scale, self.v_scale, self.ids, self.weights = k, v, k_scale, v_scale, ids, weights
         codes, blocks = (n, heads, cap, dim), (n, heads, cap // 64)
         f32, i32 = torch.float32, torch.int32
-        self.desc = CacheDesc(n, heads, dim, cap, _dense(k, codes, torch.int8, k.device, "k"),
-                              _dense(v, codes, torch.int8, k.device, "v"), _dense(k_scale, blocks, f32, k.device, "k_scale"),
-                              _dense(v_scale, blocks, f32, k.device, "v_scale"), _dense(ids, codes[:3], i32, k.device, "ids"),
-                              _dense(weights, codes[:3], f32, k.device, "weights"))
+        self.desc = CacheDesc(n, heads, dim, cap, _dense(k, codes, torch.int8, index, "k"),
+                              _dense(v, codes, torch.int8, index, "v"), _dense(k_scale, blocks, f32, index, "k_scale"),
+                              _dense(v_scale, blocks, f32, index, "v_scale"), _dense(ids, codes[:3], i32, index, "ids"),
+                              _dense(weights, codes[:3], f32, index, "weights"))
         self.batch, self.num_kv_heads, self.capacity, self.head_dim = n, heads, cap, dim
         self.status = torch.zeros(1, dtype=i32, device=k.device)
         self._attend_ws = self._evict_ws = None
@@ -416,7 +418,7 @@ class Cache:
                    new(*codes[:2], cap // 64), new(codes[:3], dtype=torch.int32), new(codes[:3]))
 
     def _count(self, t, what):
-        return None if t is None else _dense(t, (self.batch,), self.torch.int32, self.device, what)
+        return None if t is None else _dense(t, (self.batch,), self.torch.int32, self._index, what)
 
     def _workspace(self, ws, nbytes):
         if ws is None or ws.numel() < nbytes + 256:
@@ -426,13 +428,13 @@ class Cache:
     def store(self, k, v, cu, start=None, pos=None):
         """Rows cu[s] .. cu[s+1]-1 of k and v ([tokens, kv heads, dim]) go behind the start[s] rows of sequence s."""
         dt = _dtype_of(k)
-        kp, ks = _rows_view(k, self.num_kv_heads, self.head_dim, k.dtype, self.device, "k")
-        vp, vs = _rows_view(v, self.num_kv_heads, self.head_dim, k.dtype, self.device, "v")
+        kp, ks = _rows_view(k, self.num_kv_heads, self.head_dim, k.dtype, self._index, "k")
+        vp, vs = _rows_view(v, self.num_kv_heads, self.head_dim, k.dtype, self._index, "v")
         if v.shape[0] != k.shape[0]:
             raise ValueError("k and v have different numbers of rows")
-        st3_cache_store(self.desc, kp, vp, dt, ks, vs, _dense(cu, (self.batch + 1,), self.torch.int32, self.device, "cu"),
+        st3_cache_store(self.desc, kp, vp, dt, ks, vs, _dense(cu, (self.batch + 1,), self.torch.int32, self._index, "cu"),
                         k.shape[0], self._count(start, "start"), self._count(pos, "pos"), self.status.data_ptr(),
-                        _stream_of(k))
+                        _stream_of(self._index))
 
     def attend(self, q, held, out, weights_out=None, weights_in=None):
         """q and out [batch, heads, dim]; weights_out (e.g. this cache's `weights`) gets weights_in (None: this cache's)
@@ -441,15 +443,15 @@ class Cache:
         shape = (self.batch, heads, self.head_dim)
         wi = wo = None
         if weights_out is not None:
-            wi = _dense(self.weights if weights_in is None else weights_in, self.weights.shape, self.torch.float32, self.device, "weights_in")
-            wo = _dense(weights_out, self.weights.shape, self.torch.float32, self.device, "weights_out")
+            wi = _dense(self.weights if weights_in is None else weights_in, self.weights.shape, self.torch.float32, self._index, "weights_in")
+            wo = _dense(weights_out, self.weights.shape, self.torch.float32, self._index, "weights_out")
         key = (heads, wo is not None)
         if key not in self._attend_bytes:
             self._attend_bytes[key] = st3_cache_attend_workspace(self.desc, *key)
         self._attend_ws, ws = self._workspace(self._attend_ws, self._attend_bytes[key])
-        st3_cache_attend(self.desc, _dense(q, shape, q.dtype, self.device, "q"), _dense(out, shape, q.dtype, self.device, "out"),
+        st3_cache_attend(self.desc, _dense(q, shape, q.dtype, self._index, "q"), _dense(out, shape, q.dtype, self._index, "out"),
                          dt, heads, self._count(held, "held"), wi, wo, ws, self._attend_bytes[key], self.status.data_ptr(),
-                         _stream_of(q))
+                         _stream_of(self._index))
 
     def evict(self, held, seen, keep, recent=0, into=None, held_out=None):
         """Cuts every head to `keep` rows, in place or into another Cache; returns the new numbers of rows held."""
@@ -460,17 +462,19 @@ class Cache:
             self._evict_bytes = st3_cache_evict_workspace(self.desc)
         self._evict_ws, ws = self._workspace(self._evict_ws, self._evict_bytes)
         st3_cache_evict(self.desc, to.desc, self._count(held, "held"), self._count(seen, "seen"), keep, recent,
-                        self._count(held_out, "held_out"), ws, self._evict_bytes, self.status.data_ptr(), _stream_of(held))
+                        self._count(held_out, "held_out"), ws, self._evict_bytes, self.status.data_ptr(), _stream_of(self._index))
         return held_out
 
     def rows(self, held, num_rows, first=None, dtype=None):
         """(k, v, ids, weights) of rows first[s] .. first[s] + num_rows - 1 as values; rows that are not held read as 0."""
         t = self.torch
         shape = (self.batch, self.num_kv_heads, num_rows)
-        k, v = (t.empty(shape + (self.head_dim,), dtype=dtype or t.bfloat16, device=self.device) for _ in range(2))
-        ids, weights = t.empty(shape, dtype=t.int32, device=self.device), t.empty(shape, device=self.device)
+        like = self.weights.new_empty
+        both = like((2,) + shape + (self.head_dim,), dtype=dtype or t.bfloat16)
+        k, v = both[0], both[1]
+        ids, weights = self.ids.new_empty(shape), like(shape)
         st3_cache_rows(self.desc, self._count(first, "first"), self._count(held, "held"), num_rows, k.data_ptr(),
-                       v.data_ptr(), _dtype_of(k), ids.data_ptr(), weights.data_ptr(), _stream_of(k))
+                       v.data_ptr(), _dtype_of(k), ids.data_ptr(), weights.data_ptr(), _stream_of(self._index))
         return k, v, ids, weights
 
 

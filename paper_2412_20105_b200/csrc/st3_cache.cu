@@ -53,7 +53,8 @@ struct CacheView {
 };
 
 // ------------------------------------------------------------------------------------------------------------------
-// Rows in.  One thread block per (64-row block that receives rows, head, K or V).
+// Rows in.  One thread block per (64-row block that receives rows, head), for K and V together: a block's life is a chain of
+// round trips (offsets, rows, codes), and what hides it is the bytes that the blocks of an SM have under way.
 // ------------------------------------------------------------------------------------------------------------------
 struct StoreParams {
   CacheView c;
@@ -68,14 +69,25 @@ struct StoreParams {
 
 constexpr int kStoreThreads = 256;
 
-// 8 elements of a row as floats, with what is not finite as 0 (and noted in `bad`)
+// 8 elements of a row as they come
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8], bool& bad) {
+struct Raw8 { uint4 w[sizeof(T) / 2]; };
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T* p) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const uint4*>(p)[i];
+  return r;
+}
+// the same as floats, with what is not finite as 0 (and noted in `bad`)
+template <typename T>
+__device__ __forceinline__ void values8(const Raw8<T>& r, float (&f)[8], bool& bad) {
   if constexpr (sizeof(T) == 2) {
-    unpack16(*reinterpret_cast<const uint4*>(p), f);
+    unpack16(r.w[0], f);
   } else {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    const unsigned u[8] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w, r.w[1].x, r.w[1].y, r.w[1].z, r.w[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -87,10 +99,10 @@ __device__ __forceinline__ void load8(const T* p, float (&f)[8], bool& bad) {
 template <typename T, int D>
 __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const StoreParams p) {
   constexpr int kLanes = D / 8, kPass = kStoreThreads / kLanes, kIter = kBlockRows / kPass;
-  __shared__ float s_max[kStoreThreads / 32];
+  __shared__ float s_max[2][kStoreThreads / 32];
   pdl_wait();
   pdl_next();
-  const int tid = threadIdx.x, slot = blockIdx.x, head = blockIdx.y, side = blockIdx.z;
+  const int tid = threadIdx.x, slot = blockIdx.x, head = blockIdx.y;
   int below = 0;   // sequences whose first number is at most `slot`
   for (int b0 = 0; b0 < p.c.batch; b0 += kStoreThreads) {
     const int b = b0 + tid;
@@ -98,7 +110,7 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
   }
   const int b = below - 1;
   if (b < 0) return;
-  const int c0 = p.cu[b], c1 = p.cu[b + 1], start = p.start ? p.start[b] : 0;
+  const int c0 = p.cu[b], c1 = p.cu[b + 1], start = p.start ? p.start[b] : 0, pos = p.pos ? p.pos[b] : start;
   const int n = c1 - c0;
   if (n == 0) return;
   if (n < 0 || c0 < 0 || c1 > p.total || start < 0 || start > p.c.cap - n) {   // reported, nothing stored
@@ -110,55 +122,73 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
   if (row0 >= start + n) return;
   const int lo = max(start - row0, 0), hi = min(start + n - row0, kBlockRows);   // new rows of this block
   const size_t bh = (size_t)b * p.c.heads + head;
-  int8_t* codes = p.c.code[side] + (bh * p.c.cap + row0) * D;
-  float* scale = p.c.scale[side] + bh * (p.c.cap / kBlockRows) + blk;
-  const T* src = static_cast<const T*>(p.src[side]) + (long long)(c0 + row0 - start) * p.token_stride[side] +
-                 (long long)head * p.head_stride[side];
   const int lane8 = (tid % kLanes) * 8, r0 = tid / kLanes;
-  float x[kIter][8];
-  float amax = 0.f;
+  Raw8<T> raw[2][kIter];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const T* src = static_cast<const T*>(p.src[side]) + (long long)(c0 + row0 - start) * p.token_stride[side] +
+                   (long long)head * p.head_stride[side] + lane8;
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      const int r = r0 + i * kPass;
+      if (r >= lo && r < hi) raw[side][i] = load8(src + (long long)r * p.token_stride[side]);
+    }
+  }
+  float was[2];   // read ahead of the barrier, written after it
+#pragma unroll
+  for (int side = 0; side < 2; ++side) was[side] = lo > 0 ? p.c.scale[side][bh * (p.c.cap / kBlockRows) + blk] : 0.f;
+  float amax[2] = {0.f, 0.f};
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < kIter; ++i) {
-    const int r = r0 + i * kPass;
-    if (r >= lo && r < hi) {
-      load8(src + (long long)r * p.token_stride[side] + lane8, x[i], bad);
+  for (int side = 0; side < 2; ++side) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[i][e]));
+    for (int i = 0; i < kIter; ++i) {
+      const int r = r0 + i * kPass;
+      if (r >= lo && r < hi) {
+        float f[8];
+        values8(raw[side][i], f, bad);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax[side] = fmaxf(amax[side], fabsf(f[e]));
+      }
     }
+    amax[side] = warp_max(amax[side]);
+    if ((tid & 31) == 0) s_max[side][tid >> 5] = amax[side];
   }
-  const float was = lo > 0 ? *scale : 0.f;   // read ahead of the barrier, written after it
-  amax = warp_max(amax);
-  if ((tid & 31) == 0) s_max[tid >> 5] = amax;
   if (__syncthreads_or(bad) && tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
 #pragma unroll
-  for (int i = 0; i < kStoreThreads / 32; ++i) amax = fmaxf(amax, s_max[i]);
-  int e = block_exp(amax);
-  const int e_was = scale_exp(was);
-  if (lo > 0) e = max(e, e_was);
-  const float inv = exp2i(-e);
+  for (int side = 0; side < 2; ++side) {
 #pragma unroll
-  for (int i = 0; i < kIter; ++i) {
-    const int r = r0 + i * kPass;
-    uint2* at = reinterpret_cast<uint2*>(codes + r * D + lane8);
-    if (r >= lo && r < hi) {
-      int c[8];
+    for (int i = 0; i < kStoreThreads / 32; ++i) amax[side] = fmaxf(amax[side], s_max[side][i]);
+    int e = block_exp(amax[side]);
+    const int e_was = scale_exp(was[side]);
+    if (lo > 0) e = max(e, e_was);
+    const float inv = exp2i(-e);
+    int8_t* codes = p.c.code[side] + (bh * p.c.cap + row0) * D;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) c[j] = code_of(x[i][j], inv);
-      *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
-    } else if (r < lo && e > e_was) {
-      const uint2 w = *at;
-      const float f = exp2i(max(e_was - e, -126));
-      int c[8];
+    for (int i = 0; i < kIter; ++i) {
+      const int r = r0 + i * kPass;
+      uint2* at = reinterpret_cast<uint2*>(codes + r * D + lane8);
+      if (r >= lo && r < hi) {
+        float f[8];
+        values8(raw[side][i], f, bad);
+        int c[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) c[j] = code_of((float)byte_of(j < 4 ? w.x : w.y, j & 3), f);
-      *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+        for (int j = 0; j < 8; ++j) c[j] = code_of(f[j], inv);
+        *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+      } else if (r < lo && e > e_was) {
+        const uint2 w = *at;
+        const float f = exp2i(max(e_was - e, -126));
+        int c[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] = code_of((float)byte_of(j < 4 ? w.x : w.y, j & 3), f);
+        *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+      }
     }
+    if (tid == 0) p.c.scale[side][bh * (p.c.cap / kBlockRows) + blk] = exp2i(e);
   }
-  if (tid == 0) *scale = exp2i(e);
-  if (side == 0 && tid >= lo && tid < hi) {
+  if (tid >= lo && tid < hi) {
     const size_t at = bh * p.c.cap + row0 + tid;
-    p.c.ids[at] = (p.pos ? p.pos[b] : start) + row0 + tid - start;
+    p.c.ids[at] = pos + row0 + tid - start;
     p.c.weights[at] = 0.f;
   }
 }
@@ -280,13 +310,12 @@ __device__ __forceinline__ int block_sum_below(int x, int* s_warp, int& total) {
   return before + v - x;
 }
 
-// The `want`-th element in descending order (1-based) of keys whose bits above `shift + bits` equal `prefix`: finds the bin
-// of the next `bits` bits and subtracts what lies above it.  All threads return the same.
+// In a histogram: the bin that holds the want-th element from the top (1-based), its place in the bin and how many it shares
+// that with.  All threads return the same.
 struct Pick { unsigned bin; int want; int in_bin; };
 
 __device__ __forceinline__ Pick pick_bin(const int* s_hist, int bins, int want, int* s_warp, int* s_out) {
-  // thread t sums the bins [t*per, ...) counted from the top
-  const int per = bins / kEvictThreads;
+  const int per = bins / kEvictThreads;   // thread t sums the bins from t * per on, counted from the top
   int mine = 0;
   for (int j = 0; j < per; ++j) mine += s_hist[bins - 1 - (threadIdx.x * per + j)];
   int total;
@@ -305,14 +334,27 @@ __device__ __forceinline__ Pick pick_bin(const int* s_hist, int bins, int want, 
   return r;
 }
 
+constexpr int kEvictStage = 8192;    // rows whose weight and position a block keeps in shared memory
+constexpr int kEvictDirect = 512;    // rows at the cut that are ranked one against the other
+constexpr int kEvictSmem = kEvictStage * 8;
+
+// Finds the last row that stays: by a histogram of the leading 11 bits of the weights' keys and, as its bin rarely holds many,
+// by ranking the rows in that bin directly, positions included; else by the remaining bits, 11 and 10 at a time, of keys and then of
+// positions.
 __global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const EvictParams p) {
+  extern __shared__ __align__(16) unsigned char dyn[];
+  unsigned* s_key = reinterpret_cast<unsigned*>(dyn);
+  int* s_id = reinterpret_cast<int*>(dyn) + kEvictStage;
   __shared__ int s_hist[kBins];
+  __shared__ u64 s_at_cut[kEvictDirect];
   __shared__ int s_warp[kEvictThreads / 32];
   __shared__ int s_out[3];
+  __shared__ u64 s_last;
   pdl_wait();
   pdl_next();
   const int tid = threadIdx.x, bh = blockIdx.x, b = bh / p.from.heads;
   const int raw = p.held[b];
+  const int border = p.seen[b] - p.recent;   // the first position that counts as recent
   const int n = clamp_rows(raw, p.from.cap), k = min(n, p.keep);
   const int blocks = p.from.cap / kBlockRows;
   if (tid == 0) {
@@ -331,55 +373,72 @@ __global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const E
   }
   const float* w = p.from.weights + (size_t)bh * p.from.cap;
   const int* ids = p.from.ids + (size_t)bh * p.from.cap;
-  const int border = p.seen[b] - p.recent;   // the first position that counts as recent
-  // the key of the k-th row from the top, 11 + 11 + 10 bits at a time
-  unsigned prefix = 0;
-  int want = k, ties = 0;
+  const bool staged = n <= kEvictStage;
   bool nan = false;
-  const int shifts[3] = {21, 10, 0};
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = shifts[pass], bits = pass < 2 ? 11 : 10;
-    for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
+  if (tid == 0) s_out[0] = 0;
+  for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
+  __syncthreads();
+#pragma unroll 4
+  for (int i = tid; i < n; i += kEvictThreads) {
+    const float wi = w[i];
+    const int id = ids[i];
+    nan |= wi != wi;
+    const unsigned key = weight_key(wi, id >= border);
+    if (staged) { s_key[i] = key; s_id[i] = id; }
+    atomicAdd(&s_hist[key >> 21], 1);
+  }
+  auto row_key = [&](int i, int& id) {
+    id = staged ? s_id[i] : ids[i];
+    return staged ? s_key[i] : weight_key(w[i], id >= border);
+  };
+  if (__syncthreads_or(nan) && tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
+  Pick cutting = pick_bin(s_hist, kBins, k, s_warp, s_out);
+  // composite order of a row: its key, then the earlier position
+  auto composite = [](unsigned key, int id) { return ((u64)key << 32) | (unsigned)~((unsigned)id ^ 0x80000000u); };
+  u64 last;   // of the last row that stays
+  if (cutting.in_bin <= kEvictDirect) {
+    if (tid == 0) { s_out[0] = 0; s_last = 0; }
     __syncthreads();
     for (int i = tid; i < n; i += kEvictThreads) {
-      const float wi = w[i];
-      nan |= wi != wi;
-      const unsigned key = weight_key(wi, ids[i] >= border);
-      if (pass == 0 || (key >> (shift + bits)) == prefix) atomicAdd(&s_hist[(key >> shift) & ((1u << bits) - 1)], 1);
+      int id;
+      const unsigned key = row_key(i, id);
+      if ((key >> 21) == cutting.bin) s_at_cut[atomicAdd(&s_out[0], 1)] = composite(key, id);
     }
     __syncthreads();
-    const Pick r = pick_bin(s_hist, pass < 2 ? 2048 : 1024, want, s_warp, s_out);
-    prefix = (prefix << bits) | r.bin;
-    want = r.want;
-    ties = r.in_bin;
-  }
-  const unsigned cut = prefix;   // rows above it stay, `want` of the `ties` rows at it do: those of the lowest positions
-  if (__syncthreads_or(nan) && tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
-  unsigned last = 0xffffffffu;   // the last position that stays at the cut
-  if (want < ties) {
-    unsigned pre = 0;
-    for (int pass = 0; pass < 3; ++pass) {   // the want-th smallest position = the want-th largest complement
-      const int shift = shifts[pass], bits = pass < 2 ? 11 : 10;
+    if (tid < cutting.in_bin) {
+      const u64 mine = s_at_cut[tid];
+      int above = 0;
+#pragma unroll 8
+      for (int i = 0; i < cutting.in_bin; ++i) above += s_at_cut[i] > mine;
+      if (above == cutting.want - 1) s_last = mine;
+    }
+    __syncthreads();
+    last = s_last;
+  } else {
+    u64 prefix = cutting.bin;
+    int want = cutting.want;
+    const int shifts[5] = {42, 32, 21, 10, 0};   // of the composite, after its first 11 bits
+    for (int pass = 0; pass < 5; ++pass) {
+      const int shift = shifts[pass], bits = (pass == 0 ? 53 : shifts[pass - 1]) - shift;
       for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
       __syncthreads();
       for (int i = tid; i < n; i += kEvictThreads) {
-        const int id = ids[i];
-        if (weight_key(w[i], id >= border) == cut) {
-          const unsigned key = ~((unsigned)id ^ 0x80000000u);
-          if (pass == 0 || (key >> (shift + bits)) == pre) atomicAdd(&s_hist[(key >> shift) & ((1u << bits) - 1)], 1);
-        }
+        int id;
+        const unsigned key = row_key(i, id);
+        const u64 c = composite(key, id);
+        if ((c >> (shift + bits)) == prefix) atomicAdd(&s_hist[(unsigned)(c >> shift) & ((1u << bits) - 1)], 1);
       }
       __syncthreads();
-      const Pick r = pick_bin(s_hist, pass < 2 ? 2048 : 1024, want, s_warp, s_out);
-      pre = (pre << bits) | r.bin;
+      const Pick r = pick_bin(s_hist, bits == 11 ? 2048 : 1024, want, s_warp, s_out);
+      prefix = (prefix << bits) | r.bin;
       want = r.want;
     }
-    last = ~pre;
+    last = prefix;
   }
   auto stays = [&](int i) {
-    const int id = ids[i];
-    const unsigned key = weight_key(w[i], id >= border);
-    return key > cut || (key == cut && ((unsigned)id ^ 0x80000000u) <= last);
+    int id;
+    const unsigned key = row_key(i, id);
+    return composite(key, id) >= last;
   };
   // rows behind the new length that stay, in order
   int* movers = p.movers + (size_t)bh * p.from.cap;
@@ -419,22 +478,16 @@ __global__ void __launch_bounds__(kMoveThreads) st3_cache_move_kernel(const Evic
   pdl_wait();
   pdl_next();
   const int tid = threadIdx.x, bh = blockIdx.y, blk = blockIdx.x;
-  const int k = p.length[bh], row0 = blk * kBlockRows;
+  const int from_blocks = p.from.cap / kBlockRows, row0 = blk * kBlockRows;
+  // one round trip for all three; what `mine` holds behind the new length is not used
+  const int k = p.length[bh];
+  const bool changed = p.changed[(size_t)bh * from_blocks + blk];
+  const int mine = tid < kBlockRows ? p.src[(size_t)bh * p.from.cap + row0 + tid] : 0;
   if (blk == 0 && bh % p.from.heads == 0 && tid == 0) p.held_out[bh / p.from.heads] = k;
   if (row0 >= k) return;
-  const int from_blocks = p.from.cap / kBlockRows;
-  const bool changed = p.changed[(size_t)bh * from_blocks + blk];
   if (p.in_place && !changed) return;
   const int rows = min(k - row0, kBlockRows);
-  if (tid < kBlockRows) {
-    const int s = tid < rows ? p.src[(size_t)bh * p.from.cap + row0 + tid] : 0;
-    s_src[tid] = s;
-    // in place the scale of the block that the new length cuts may already be that of the rows moved into it
-    const bool edge = s >= k && s / kBlockRows == k / kBlockRows;
-#pragma unroll
-    for (int side = 0; side < 2; ++side)
-      s_scale[side][tid] = edge ? p.edge[2 * bh + side] : p.from.scale[side][(size_t)bh * from_blocks + s / kBlockRows];
-  }
+  if (tid < kBlockRows) s_src[tid] = tid < rows ? mine : 0;
   __syncthreads();
   uint4 piece[2][kIter];
   float amax[2] = {0.f, 0.f};
@@ -445,6 +498,19 @@ __global__ void __launch_bounds__(kMoveThreads) st3_cache_move_kernel(const Evic
       const int at = tid + i * kMoveThreads, r = at / kLanes, col = (at % kLanes) * 16;
       if (r < rows) piece[side][i] = *reinterpret_cast<const uint4*>(p.from.code[side] + ((size_t)bh * p.from.cap + s_src[r]) * D + col);
     }
+  int id = 0;
+  float weight = 0.f;
+  if (tid < kBlockRows) {
+    const int s = s_src[tid];
+    // in place the scale of the block that the new length cuts may already be that of the rows moved into it
+    const bool edge = s >= k && s / kBlockRows == k / kBlockRows;
+#pragma unroll
+    for (int side = 0; side < 2; ++side)
+      s_scale[side][tid] = edge ? p.edge[2 * bh + side] : p.from.scale[side][(size_t)bh * from_blocks + s / kBlockRows];
+    id = p.from.ids[(size_t)bh * p.from.cap + s];
+    weight = p.from.weights[(size_t)bh * p.from.cap + s];
+  }
+  __syncthreads();
 #pragma unroll
   for (int side = 0; side < 2; ++side)
 #pragma unroll
@@ -493,9 +559,9 @@ __global__ void __launch_bounds__(kMoveThreads) st3_cache_move_kernel(const Evic
     if (tid == 0) p.to.scale[side][(size_t)bh * to_blocks + blk] = exp2i(e);
   }
   if (tid < rows) {
-    const size_t from = (size_t)bh * p.from.cap + s_src[tid], to = (size_t)bh * p.to.cap + row0 + tid;
-    p.to.ids[to] = p.from.ids[from];
-    p.to.weights[to] = p.from.weights[from];
+    const size_t to = (size_t)bh * p.to.cap + row0 + tid;
+    p.to.ids[to] = id;
+    p.to.weights[to] = weight;
   }
 }
 
@@ -558,7 +624,7 @@ extern "C" st3_status st3_cache_store(const st3_cache* cache, const void* k, con
   p.token_stride[0] = k_token_stride; p.token_stride[1] = v_token_stride;
   p.head_stride[0] = k_head_stride; p.head_stride[1] = v_head_stride;
   p.cu = cu; p.start = start; p.pos = pos; p.status = dev_status; p.total = total;
-  const dim3 grid((unsigned)(total / kBlockRows + 2 * cache->batch), (unsigned)cache->num_kv_heads, 2);
+  const dim3 grid((unsigned)(total / kBlockRows + 2 * cache->batch), (unsigned)cache->num_kv_heads);
   const dim3 block(kStoreThreads);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (dtype == ST3_BF16)
@@ -645,7 +711,8 @@ extern "C" st3_status st3_cache_evict(const st3_cache* from, const st3_cache* to
   p.keep = keep; p.recent = recent; p.in_place = same == 6;
   const unsigned bh = (unsigned)(from->batch * from->num_kv_heads);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  st = launch(st3_cache_select_kernel, dim3(bh), dim3(kEvictThreads), 0, s, p);
+  if (!allow_smem<st3_cache_select_kernel>(kEvictSmem)) return ST3_ERR_CUDA;
+  st = launch(st3_cache_select_kernel, dim3(bh), dim3(kEvictThreads), kEvictSmem, s, p);
   if (st != ST3_OK) return st;
   const int most = keep < from->capacity ? keep : from->capacity;
   const dim3 grid((unsigned)((most + kBlockRows - 1) / kBlockRows), bh);
@@ -686,12 +753,11 @@ bool make_code_map(EncodeTiledFn fn, CUtensorMap* map, const st3_cache* c, const
 
 template <typename T, int D, int kTiles>
 st3_status attend_launch(const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttendParams& p, cudaStream_t s) {
-  if (cudaFuncSetAttribute(st3_cache_attend_kernel<T, D, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, CaLayout<D>::kTotal) != cudaSuccess)
-    return ST3_ERR_CUDA;
+  if (!allow_smem<st3_cache_attend_kernel<T, D, kTiles>>(CaLayout<D>::kTotal)) return ST3_ERR_CUDA;
   st3_status st = launch(st3_cache_attend_kernel<T, D, kTiles>, dim3((unsigned)p.grid), dim3(kCaThreads), CaLayout<D>::kTotal, s, mk, mv, p);
   if (st != ST3_OK) return st;
   const unsigned chunks = p.weights_out ? (unsigned)((p.c.cap + kCaChunk - 1) / kCaChunk) : 0u;
-  return launch(st3_cache_merge_kernel<T, D>, dim3((unsigned)(p.c.batch * p.c.heads), (unsigned)p.passes + chunks), dim3(kCaMergeThreads), 0, s, p);
+  return launch(st3_cache_merge_kernel<T, D>, dim3((unsigned)(p.c.batch * p.c.heads), (unsigned)p.group + chunks), dim3(kCaMergeThreads), 0, s, p);
 }
 
 st3_status check_heads(const st3_cache* c, int heads) {
@@ -699,7 +765,7 @@ st3_status check_heads(const st3_cache* c, int heads) {
   if (heads / c->num_kv_heads > 1024 || (long long)c->batch * heads * c->capacity > 0x7fffffffffLL) return ST3_ERR_UNSUPPORTED;
   const long long passes = (heads / c->num_kv_heads + kCaHeads - 1) / kCaHeads;
   if ((long long)c->batch * c->num_kv_heads * passes * (c->capacity / kBlockRows) > 0x3fffffffLL) return ST3_ERR_UNSUPPORTED;
-  if (passes + c->capacity / kCaChunk + 1 > 65535) return ST3_ERR_UNSUPPORTED;
+  if (heads / c->num_kv_heads + c->capacity / kCaChunk + 1 > 65535) return ST3_ERR_UNSUPPORTED;
   return ST3_OK;
 }
 

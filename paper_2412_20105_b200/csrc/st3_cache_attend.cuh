@@ -25,8 +25,8 @@ constexpr int kCaGrid = 2 * 148;       // one wave
 constexpr int kCaConsumers = 4;
 constexpr int kCaThreads = (kCaConsumers + 1) * 32;
 constexpr int kCaHeads = 16;           // query heads of one pass over a group's rows; larger groups take several
-constexpr int kCaChunk = 1024;         // rows of the second launch's blocks that add weights
-constexpr int kCaMergeThreads = 256;
+constexpr int kCaChunk = 512;          // rows of the second launch's blocks that add weights
+constexpr int kCaMergeThreads = 128;
 
 struct CacheAttendParams {
   CacheView c;
@@ -251,6 +251,12 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const size_t bh = (size_t)b * p.c.heads + head;
     const float* ks = p.c.scale[0] + bh * (p.c.cap / kBlockRows);
     const float* vs = p.c.scale[1] + bh * (p.c.cap / kBlockRows);
+    float ks32, vs32;   // the scales of 32 blocks, one a lane; requested ahead of the queries
+    {
+      const int j = min(i0 + lane, i1 - 1);
+      ks32 = ks[j];
+      vs32 = vs[j];
+    }
     // ---- the queries of this pass as B fragments: lane (g, t) holds head g, dims 16 i + 4 t .. + 3 ----
     uint32_t qf[kTerms][kTiles][kSteps][2];
     float qs[kTiles][2];   // factor of the logits of heads 2 t and 2 t + 1
@@ -305,10 +311,9 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
     }
-    float ks32 = 0.f, vs32 = 0.f;   // the scales of 32 blocks, one a lane
     for (int i = i0; i < i1; ++i) {
       const int at = (i - i0) & 31;
-      if (at == 0) {
+      if (at == 0 && i > i0) {
         const int j = min(i + lane, i1 - 1);
         ks32 = ks[j];
         vs32 = vs[j];
@@ -354,9 +359,14 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         for (int e = 0; e < 4; ++e) v[e] = ((e < 2) ? in0 : in1) ? (s[n][e] + s2[n][e]) * (kscale * qs[n][e & 1]) : -INFINITY;
         if (p.logits) {
           float* dst = p.logits + ((size_t)bh * p.c.cap + row) * p.group + h0 + n * 8 + 2 * t;
+          if (p.group & 1) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (((e < 2) ? in0 : in1) && n * 8 + 2 * t + (e & 1) < heads) dst[(e >> 1) * 8 * p.group + (e & 1)] = v[e];
+            for (int e = 0; e < 4; ++e)
+              if (((e < 2) ? in0 : in1) && n * 8 + 2 * t + (e & 1) < heads) dst[(e >> 1) * 8 * p.group + (e & 1)] = v[e];
+          } else if (n * 8 + 2 * t < heads) {   // pairs of heads side by side, on 8 bytes
+            if (in0) *reinterpret_cast<float2*>(dst) = make_float2(v[0], v[1]);
+            if (in1) *reinterpret_cast<float2*>(dst + 8 * p.group) = make_float2(v[2], v[3]);
+          }
         }
         float top[2] = {fmaxf(v[0], v[2]), fmaxf(v[1], v[3])};
 #pragma unroll
@@ -492,33 +502,27 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   }
 }
 
-// Joins the partials of a (sequence, key/value head) into the output (grid y = 0 .. passes - 1), and adds the probabilities
-// of its rows to their weights (the other y, kCaChunk rows each).
+// Joins the partials.  Grid y < group: the output of one head (a block of four warps, each with every fourth segment's sums);
+// the other y: kCaChunk rows of a (sequence, key/value head), whose weights get the probabilities of the group's heads.
+// Bound by round trips: the row counts are read before the wait (the attention launch ahead has started only after everything
+// before it was complete, and leaves them alone); a head's maxima and sums are requested together with the sums of its
+// outputs, or with the logits (a block to a (sequence, head) that did one after the other: 16 -> 7 us for 32 sequences).
 template <typename T, int D>
 __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const CacheAttendParams p) {
-  __shared__ int s_sum[2][kCaMergeThreads / 32];
+  constexpr int kWarps4 = kCaMergeThreads / 32, kAhead = 8, kVec = D / 32;
+  __shared__ int s_sum[2][kWarps4];
+  __shared__ float s_ml[3][kCaGrid + 1];
   __shared__ float s_ref[128], s_inv[128];
-  __shared__ float s_acc[kCaMergeThreads / 32][D];
-  pdl_wait();
-  pdl_next();
+  __shared__ float s_acc[kWarps4][D];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x;
   const int b = bh / p.c.heads, head = bh - b * p.c.heads, pairs = p.c.heads * p.passes;
-  const int held = clamp_rows(p.held[b], p.c.cap), nb = (held + kBlockRows - 1) / kBlockRows;
-  const bool weigh = (int)blockIdx.y >= p.passes;
-  const int row0 = ((int)blockIdx.y - p.passes) * kCaChunk;
-  if (weigh && row0 >= held) return;
-  if (nb == 0) {
-    T* out = static_cast<T*>(p.out) + ((size_t)bh * p.group + blockIdx.y * kCaHeads) * D;
-    const int n = min(p.group - (int)blockIdx.y * kCaHeads, kCaHeads) * D;
-    for (int i = tid; i < n; i += kCaMergeThreads) store_out(out + i, 0.f);
-    return;
-  }
   int all = 0, below = 0;
   for (int i = tid; i < p.c.batch; i += kCaMergeThreads) {
     const int n = blocks_of(p, i);
     all += n;
     if (i < b) below += n;
   }
+  const int held = clamp_rows(p.held[b], p.c.cap), nb = (held + kBlockRows - 1) / kBlockRows;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     all += __shfl_xor_sync(0xffffffffu, all, o);
@@ -528,102 +532,137 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
   __syncthreads();
   all = below = 0;
 #pragma unroll
-  for (int w = 0; w < kCaMergeThreads / 32; ++w) { all += s_sum[0][w]; below += s_sum[1][w]; }
+  for (int w = 0; w < kWarps4; ++w) { all += s_sum[0][w]; below += s_sum[1][w]; }
   const int total = all * pairs, grid = min(p.grid, total);
-  constexpr int kWarps8 = kCaMergeThreads / 32;
-  if (!weigh) {
-    const int pass = blockIdx.y, pair = head * p.passes + pass;
-    const int heads = min(p.group - pass * kCaHeads, kCaHeads);
-    const int x = (below * pairs) + pair * nb;
-    const int c0 = run_of(total, x, grid), c1 = run_of(total, x + nb - 1, grid);
-    const size_t slot0 = (size_t)b * pairs + pair;
-    // warps to a head, and the segments that each of them takes
-    const int split = heads >= kWarps8 ? 1 : kWarps8 / heads;
-    for (int h = warp / split; h < (heads + kWarps8 - 1) / kWarps8 * kWarps8; h += kWarps8 / split) {
-      const bool live = h < heads && warp / split < kWarps8 / split;
-      const int part = warp % split;
-      float a = -INFINITY, av = -INFINITY, sum = 0.f;
-      float o[D / 32];
+  pdl_wait();
+  pdl_next();
+  if ((int)blockIdx.y < p.group) {
+    // ---- one head's output ----
+    const int h = blockIdx.y, pass = h / kCaHeads, pair = head * p.passes + pass;
+    T* dst = static_cast<T*>(p.out) + ((size_t)bh * p.group + h) * D;
+    if (nb == 0) {
+      if (tid < D) store_out(dst + tid, 0.f);
+      return;
+    }
+    const int x = below * pairs + pair * nb;
+    const int c0 = run_of(total, x, grid), n = run_of(total, x + nb - 1, grid) - c0 + 1;   // n <= grid segments
+    const size_t slot0 = ((size_t)b * pairs + pair + c0) * p.pitch + h - pass * kCaHeads;
+    const float* ml = p.part_ml + slot0 * 3;
+    const float* acc = p.part_acc + slot0 * D + lane * kVec;
+    float ahead[kAhead][kVec];
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-      if (live) {
-        for (int c = c0 + lane; c <= c1; c += 32) {
-          const float* ml = p.part_ml + ((slot0 + c) * p.pitch + h) * 3;
-          a = fmaxf(a, ml[0]);
-          av = fmaxf(av, ml[1]);
+    for (int j = 0; j < kAhead; ++j) {
+      const int c = warp + j * kWarps4;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) ahead[j][e] = 0.f;
+      if (c < n) {
+        if constexpr (kVec == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(acc + (size_t)c * p.pitch * D);
+          ahead[j][0] = v.x; ahead[j][1] = v.y; ahead[j][kVec - 2] = v.z; ahead[j][kVec - 1] = v.w;
+        } else {
+          const float2 v = *reinterpret_cast<const float2*>(acc + (size_t)c * p.pitch * D);
+          ahead[j][0] = v.x; ahead[j][1] = v.y;
         }
-        a = warp_max(a);
-        av = warp_max(av);
-        const float ref = a > -INFINITY ? a : 0.f, refv = av > -INFINITY ? av : 0.f;
-        for (int c = c0 + lane; c <= c1; c += 32) {
-          const float* ml = p.part_ml + ((slot0 + c) * p.pitch + h) * 3;
-          sum += ml[2] * fast_exp2(ml[0] - ref);
-        }
-        sum = warp_sum(sum);
+      }
+    }
+    for (int c = tid; c < n; c += kCaMergeThreads)
+#pragma unroll
+      for (int e = 0; e < 3; ++e) s_ml[e][c] = ml[(size_t)c * p.pitch * 3 + e];
+    __syncthreads();
+    float a = -INFINITY, av = -INFINITY, sum = 0.f;
+    for (int c = lane; c < n; c += 32) { a = fmaxf(a, s_ml[0][c]); av = fmaxf(av, s_ml[1][c]); }
+    a = warp_max(a);
+    av = warp_max(av);
+    const float ref = a > -INFINITY ? a : 0.f, refv = av > -INFINITY ? av : 0.f;
+    for (int c = lane; c < n; c += 32) sum += s_ml[2][c] * fast_exp2(s_ml[0][c] - ref);
+    sum = warp_sum(sum);
+    float o[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int c = warp + j * kWarps4;
+      if (c < n) {
+        const float f = fast_exp2(s_ml[1][c] - refv);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) o[e] = fmaf(ahead[j][e], f, o[e]);
+      }
+    }
 #pragma unroll 4
-        for (int c = c0 + part; c <= c1; c += split) {
-          const float f = fast_exp2(p.part_ml[((slot0 + c) * p.pitch + h) * 3 + 1] - refv);
-          const float* src = p.part_acc + ((slot0 + c) * p.pitch + h) * D + lane * (D / 32);
-          if constexpr (D == 128) {
-            const float4 v = *reinterpret_cast<const float4*>(src);
-            o[0] += v.x * f; o[1] += v.y * f; o[D / 32 - 2] += v.z * f; o[D / 32 - 1] += v.w * f;
-          } else {
-            const float2 v = *reinterpret_cast<const float2*>(src);
-            o[0] += v.x * f; o[1] += v.y * f;
-          }
-        }
-        // sums relative to 2^refv over a denominator relative to 2^ref
-        const float inv = fast_exp2(refv - ref) / sum;
+    for (int c = warp + kAhead * kWarps4; c < n; c += kWarps4) {
+      const float f = fast_exp2(s_ml[1][c] - refv);
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] *= inv;
-      }
-      if (split > 1) {
-        __syncthreads();
+      for (int e = 0; e < kVec; ++e) o[e] = fmaf(acc[(size_t)c * p.pitch * D + e], f, o[e]);
+    }
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) s_acc[warp][lane * (D / 32) + e] = o[e];
-        __syncthreads();
-        if (live && part == 0)
-          for (int w = 1; w < split; ++w)
+    for (int e = 0; e < kVec; ++e) s_acc[warp][lane * kVec + e] = o[e];
+    __syncthreads();
+    // sums relative to 2^refv over a denominator relative to 2^ref
+    if (tid < D) {
+      float v = 0.f;
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) o[e] += s_acc[warp + w][lane * (D / 32) + e];
-      }
-      if (live && part == 0) {
-        T* dst = static_cast<T*>(p.out) + ((size_t)bh * p.group + pass * kCaHeads + h) * D + lane * (D / 32);
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) store_out(dst + e, o[e]);
-      }
-      if (split > 1) break;   // one round covers all heads
+      for (int w = 0; w < kWarps4; ++w) v += s_acc[w][tid];
+      store_out(dst + tid, v * (fast_exp2(refv - ref) / sum));
     }
     return;
   }
   // ---- weights ----
+  constexpr int kRowsEach = kCaChunk / kCaMergeThreads;
+  const int row0 = ((int)blockIdx.y - p.group) * kCaChunk;
+  if (row0 >= held) return;
+  const float* logits = p.logits + ((size_t)bh * p.c.cap + row0) * p.group;
+  float add[kRowsEach], first[kRowsEach][8];   // the weights, and the logits of the first eight heads
+#pragma unroll
+  for (int i = 0; i < kRowsEach; ++i) {
+    const int r = tid + i * kCaMergeThreads;
+    add[i] = row0 + r < held ? p.weights_in[(size_t)bh * p.c.cap + row0 + r] : 0.f;
+    if (p.group == 4) {
+      const float4 v = row0 + r < held ? reinterpret_cast<const float4*>(logits)[r] : make_float4(0.f, 0.f, 0.f, 0.f);
+      first[i][0] = v.x; first[i][1] = v.y; first[i][2] = v.z; first[i][3] = v.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) first[i][j] = j < p.group && row0 + r < held ? logits[(size_t)r * p.group + j] : 0.f;
+    }
+  }
   for (int h0 = 0; h0 < p.group; h0 += 128) {
     __syncthreads();
-    for (int h = h0 + warp; h < min(p.group, h0 + 128); h += kWarps8) {
+    for (int h = h0 + warp; h < min(p.group, h0 + 128); h += kWarps4) {
       const int pass = h / kCaHeads, pair = head * p.passes + pass;
-      const int x = (below * pairs) + pair * nb;
-      const int c0 = run_of(total, x, grid), c1 = run_of(total, x + nb - 1, grid);
-      const size_t slot0 = (size_t)b * pairs + pair;
+      const int x = below * pairs + pair * nb;
+      const int c0 = run_of(total, x, grid), n = run_of(total, x + nb - 1, grid) - c0 + 1;
+      const float* ml = p.part_ml + (((size_t)b * pairs + pair + c0) * p.pitch + h - pass * kCaHeads) * 3;
       float a = -INFINITY, sum = 0.f;
-      for (int c = c0 + lane; c <= c1; c += 32) a = fmaxf(a, p.part_ml[((slot0 + c) * p.pitch + h - pass * kCaHeads) * 3]);
-      a = warp_max(a);
-      const float ref = a > -INFINITY ? a : 0.f;
-      for (int c = c0 + lane; c <= c1; c += 32) {
-        const float* ml = p.part_ml + ((slot0 + c) * p.pitch + h - pass * kCaHeads) * 3;
-        sum += ml[2] * fast_exp2(ml[0] - ref);
+      for (int c = lane; c < n; c += 32) {   // relative to the lane's own maximum so far
+        const float m = ml[(size_t)c * p.pitch * 3], l = ml[(size_t)c * p.pitch * 3 + 2];
+        const float top = fmaxf(a, m), ref = top > -INFINITY ? top : 0.f;
+        sum = sum * fast_exp2(a - ref) + l * fast_exp2(m - ref);
+        a = top;
       }
-      sum = warp_sum(sum);
+      const float top = warp_max(a), ref = top > -INFINITY ? top : 0.f;
+      sum = warp_sum(sum * fast_exp2(a - ref));
       if (lane == 0) { s_ref[h - h0] = ref; s_inv[h - h0] = 1.f / sum; }
     }
     __syncthreads();
     const int n = min(p.group - h0, 128);
-    for (int r = row0 + tid; r < min(row0 + kCaChunk, held); r += kCaMergeThreads) {
-      const float* src = p.logits + ((size_t)bh * p.c.cap + r) * p.group + h0;
-      const size_t at = (size_t)bh * p.c.cap + r;
+#pragma unroll
+    for (int i = 0; i < kRowsEach; ++i) {
+      const int r = tid + i * kCaMergeThreads;
+      if (row0 + r >= held) continue;
       float sum = 0.f;
-      for (int j = 0; j < n; ++j) sum += fast_exp2(src[j] - s_ref[j]) * s_inv[j];
-      p.weights_out[at] = (h0 ? p.weights_out[at] : p.weights_in[at]) + sum;
+      int j = 0;
+      if (h0 == 0) {
+#pragma unroll
+        for (; j < 8; ++j)
+          if (j < n) sum += fast_exp2(first[i][j] - s_ref[j]) * s_inv[j];
+      }
+      for (; j < n; ++j) sum += fast_exp2(logits[(size_t)r * p.group + h0 + j] - s_ref[j]) * s_inv[j];
+      add[i] += sum;
     }
+  }
+#pragma unroll
+  for (int i = 0; i < kRowsEach; ++i) {
+    const int r = tid + i * kCaMergeThreads;
+    if (row0 + r < held) p.weights_out[(size_t)bh * p.c.cap + row0 + r] = add[i];
   }
 }
 

@@ -6,6 +6,8 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 namespace {
 
 // A launch that may be set up while the one ahead of it in the stream still runs; the kernel waits for it itself.
@@ -22,6 +24,20 @@ st3_status launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cuda
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? ST3_OK : ST3_ERR_CUDA;
+}
+
+// Raises a kernel's limit of dynamic shared memory, once on each device (a call costs as much as a fifth of a launch).  Two
+// first calls at once set the same value twice.
+template <auto kKernel>
+bool allow_smem(int bytes) {
+  static std::atomic<unsigned long long> devices{0};
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return false;
+  const bool known = device < 64;
+  if (known && (devices.load(std::memory_order_acquire) >> device & 1)) return true;
+  if (cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  if (known) devices.fetch_or(1ull << device, std::memory_order_release);
+  return true;
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,

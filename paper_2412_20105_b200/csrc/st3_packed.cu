@@ -879,13 +879,12 @@ PackedParams packed_params(const st3_packed* p, const int32_t* cu, int* status) 
 
 template <int D>
 st3_status attend_launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const PackedParams& d, cudaStream_t s) {
-  if (cudaFuncSetAttribute(st3_packed_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotal) != cudaSuccess) return ST3_ERR_CUDA;
+  if (!allow_smem<st3_packed_attend_kernel<D>>(PkLayout<D>::kTotal)) return ST3_ERR_CUDA;
   return launch(st3_packed_attend_kernel<D>, dim3((unsigned)d.items), dim3(AttendRoles::kThreads), PkLayout<D>::kTotal, s, mq, mk, mv, d);
 }
 template <int D>
 st3_status weights_launch(const CUtensorMap& mq, const CUtensorMap& mk, const PackedParams& d, cudaStream_t s) {
-  if (cudaFuncSetAttribute(st3_packed_weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PkLayout<D>::kTotalWeights) != cudaSuccess)
-    return ST3_ERR_CUDA;
+  if (!allow_smem<st3_packed_weights_kernel<D>>(PkLayout<D>::kTotalWeights)) return ST3_ERR_CUDA;
   return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(WeightRoles::kThreads), PkLayout<D>::kTotalWeights, s, mq, mk, d);
 }
 
