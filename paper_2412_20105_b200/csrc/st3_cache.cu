@@ -756,8 +756,13 @@ st3_status attend_launch(const CUtensorMap& mk, const CUtensorMap& mv, const Cac
   if (!allow_smem<st3_cache_attend_kernel<T, D, kTiles>>(CaLayout<D>::kTotal)) return ST3_ERR_CUDA;
   st3_status st = launch(st3_cache_attend_kernel<T, D, kTiles>, dim3((unsigned)p.grid), dim3(kCaThreads), CaLayout<D>::kTotal, s, mk, mv, p);
   if (st != ST3_OK) return st;
-  const unsigned chunks = p.weights_out ? (unsigned)((p.c.cap + kCaChunk - 1) / kCaChunk) : 0u;
-  return launch(st3_cache_merge_kernel<T, D>, dim3((unsigned)(p.c.batch * p.c.heads), (unsigned)p.group + chunks), dim3(kCaMergeThreads), 0, s, p);
+  const unsigned pairs = (unsigned)(p.c.batch * p.c.heads), group = (unsigned)p.group;
+  auto chunks = [&](int split) { return p.weights_out ? (unsigned)((p.c.cap + ca_chunk(split) - 1) / ca_chunk(split)) : 0u; };
+  const dim3 block(kCaMergeThreads);
+  // five segments a pair or more on average (the wave's thread blocks over the pairs): four warps to a head
+  if (pairs * (unsigned)p.passes * 4 <= kCaGrid)
+    return launch(st3_cache_merge_kernel<T, D, 4>, dim3(pairs, group + chunks(4)), block, 0, s, p);
+  return launch(st3_cache_merge_kernel<T, D, 1>, dim3(pairs, (group + 3) / 4 + chunks(1)), block, 0, s, p);
 }
 
 st3_status check_heads(const st3_cache* c, int heads) {
@@ -765,7 +770,7 @@ st3_status check_heads(const st3_cache* c, int heads) {
   if (heads / c->num_kv_heads > 1024 || (long long)c->batch * heads * c->capacity > 0x7fffffffffLL) return ST3_ERR_UNSUPPORTED;
   const long long passes = (heads / c->num_kv_heads + kCaHeads - 1) / kCaHeads;
   if ((long long)c->batch * c->num_kv_heads * passes * (c->capacity / kBlockRows) > 0x3fffffffLL) return ST3_ERR_UNSUPPORTED;
-  if (heads / c->num_kv_heads + c->capacity / kCaChunk + 1 > 65535) return ST3_ERR_UNSUPPORTED;
+  if (heads / c->num_kv_heads + c->capacity / ca_chunk(4) + 1 > 65535) return ST3_ERR_UNSUPPORTED;
   return ST3_OK;
 }
 

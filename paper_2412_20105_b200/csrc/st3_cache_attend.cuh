@@ -25,8 +25,9 @@ constexpr int kCaGrid = 2 * 148;       // one wave
 constexpr int kCaConsumers = 4;
 constexpr int kCaThreads = (kCaConsumers + 1) * 32;
 constexpr int kCaHeads = 16;           // query heads of one pass over a group's rows; larger groups take several
-constexpr int kCaChunk = 512;          // rows of the second launch's blocks that add weights
 constexpr int kCaMergeThreads = 128;
+// Rows of the second launch's blocks that add weights: one round of loads, or two where blocks are many.
+__host__ __device__ constexpr int ca_chunk(int split) { return split == 4 ? 512 : 1024; }
 
 struct CacheAttendParams {
   CacheView c;
@@ -143,6 +144,8 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   float* s_red = reinterpret_cast<float*>(smem + L::kRed);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
+    prefetch_map(&map_k);
+    prefetch_map(&map_v);
     for (int i = 0; i < L::kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], kCaConsumers); }
     mbar_fence_init();
     s_int[8] = 0;
@@ -502,16 +505,18 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   }
 }
 
-// Joins the partials.  Grid y < group: the output of one head (a block of four warps, each with every fourth segment's sums);
-// the other y: kCaChunk rows of a (sequence, key/value head), whose weights get the probabilities of the group's heads.
+// Joins the partials.  Grid y < out_blocks: the outputs of 4 / kSplit heads, a head's segments shared out over kSplit warps; the
+// other y: kChunk rows of a (sequence, key/value head), whose weights get the probabilities of the group's heads.
 // Bound by round trips: the row counts are read before the wait (the attention launch ahead has started only after everything
 // before it was complete, and leaves them alone); a head's maxima and sums are requested together with the sums of its
-// outputs, or with the logits (a block to a (sequence, head) that did one after the other: 16 -> 7 us for 32 sequences).
-template <typename T, int D>
+// outputs, or with the logits.  Four warps a head where a pair has many segments (4 x 65 000 rows of 8 heads: 11 -> 5 us
+// against one block for all heads), one where the pairs are many and the blocks would take several rounds of the GPU.
+template <typename T, int D, int kSplit>
 __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const CacheAttendParams p) {
-  constexpr int kWarps4 = kCaMergeThreads / 32, kAhead = 8, kVec = D / 32;
+  constexpr int kWarps4 = kCaMergeThreads / 32, kHeads = kWarps4 / kSplit, kAhead = kSplit == 4 ? 8 : 4, kVec = D / 32;
+  constexpr int kChunk = ca_chunk(kSplit);
   __shared__ int s_sum[2][kWarps4];
-  __shared__ float s_ml[3][kCaGrid + 1];
+  __shared__ float s_ml[kHeads][3][kCaGrid + 1];
   __shared__ float s_ref[128], s_inv[128];
   __shared__ float s_acc[kWarps4][D];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x;
@@ -536,23 +541,27 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
   const int total = all * pairs, grid = min(p.grid, total);
   pdl_wait();
   pdl_next();
-  if ((int)blockIdx.y < p.group) {
-    // ---- one head's output ----
-    const int h = blockIdx.y, pass = h / kCaHeads, pair = head * p.passes + pass;
+  const int out_blocks = (p.group + kHeads - 1) / kHeads;
+  if ((int)blockIdx.y < out_blocks) {
+    // ---- outputs ----
+    const int sub = warp % kSplit, h = blockIdx.y * kHeads + warp / kSplit, pass = h / kCaHeads, pair = head * p.passes + pass;
+    const bool live = h < p.group;
+    float (&mls)[3][kCaGrid + 1] = s_ml[warp / kSplit];
     T* dst = static_cast<T*>(p.out) + ((size_t)bh * p.group + h) * D;
     if (nb == 0) {
-      if (tid < D) store_out(dst + tid, 0.f);
+      if (live && sub == 0)
+        for (int e = lane; e < D; e += 32) store_out(dst + e, 0.f);
       return;
     }
     const int x = below * pairs + pair * nb;
-    const int c0 = run_of(total, x, grid), n = run_of(total, x + nb - 1, grid) - c0 + 1;   // n <= grid segments
+    const int c0 = run_of(total, x, grid), n = live ? run_of(total, x + nb - 1, grid) - c0 + 1 : 0;   // n <= grid segments
     const size_t slot0 = ((size_t)b * pairs + pair + c0) * p.pitch + h - pass * kCaHeads;
     const float* ml = p.part_ml + slot0 * 3;
     const float* acc = p.part_acc + slot0 * D + lane * kVec;
     float ahead[kAhead][kVec];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int c = warp + j * kWarps4;
+      const int c = sub + j * kSplit;
 #pragma unroll
       for (int e = 0; e < kVec; ++e) ahead[j][e] = 0.f;
       if (c < n) {
@@ -565,66 +574,73 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
         }
       }
     }
-    for (int c = tid; c < n; c += kCaMergeThreads)
+    for (int c = sub * 32 + lane; c < n; c += kSplit * 32)
 #pragma unroll
-      for (int e = 0; e < 3; ++e) s_ml[e][c] = ml[(size_t)c * p.pitch * 3 + e];
+      for (int e = 0; e < 3; ++e) mls[e][c] = ml[(size_t)c * p.pitch * 3 + e];
     __syncthreads();
     float a = -INFINITY, av = -INFINITY, sum = 0.f;
-    for (int c = lane; c < n; c += 32) { a = fmaxf(a, s_ml[0][c]); av = fmaxf(av, s_ml[1][c]); }
+    for (int c = lane; c < n; c += 32) { a = fmaxf(a, mls[0][c]); av = fmaxf(av, mls[1][c]); }
     a = warp_max(a);
     av = warp_max(av);
     const float ref = a > -INFINITY ? a : 0.f, refv = av > -INFINITY ? av : 0.f;
-    for (int c = lane; c < n; c += 32) sum += s_ml[2][c] * fast_exp2(s_ml[0][c] - ref);
+    for (int c = lane; c < n; c += 32) sum += mls[2][c] * fast_exp2(mls[0][c] - ref);
     sum = warp_sum(sum);
     float o[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) o[e] = 0.f;
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int c = warp + j * kWarps4;
+      const int c = sub + j * kSplit;
       if (c < n) {
-        const float f = fast_exp2(s_ml[1][c] - refv);
+        const float f = fast_exp2(mls[1][c] - refv);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) o[e] = fmaf(ahead[j][e], f, o[e]);
       }
     }
 #pragma unroll 4
-    for (int c = warp + kAhead * kWarps4; c < n; c += kWarps4) {
-      const float f = fast_exp2(s_ml[1][c] - refv);
+    for (int c = sub + kAhead * kSplit; c < n; c += kSplit) {
+      const float f = fast_exp2(mls[1][c] - refv);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) o[e] = fmaf(acc[(size_t)c * p.pitch * D + e], f, o[e]);
     }
+    const float inv = fast_exp2(refv - ref) / sum;   // sums relative to 2^refv over a denominator relative to 2^ref
+    if constexpr (kSplit > 1) {
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) s_acc[warp][lane * kVec + e] = o[e];
-    __syncthreads();
-    // sums relative to 2^refv over a denominator relative to 2^ref
-    if (tid < D) {
-      float v = 0.f;
+      for (int e = 0; e < kVec; ++e) s_acc[warp][lane * kVec + e] = o[e];
+      __syncthreads();
+      if (sub > 0) return;
 #pragma unroll
-      for (int w = 0; w < kWarps4; ++w) v += s_acc[w][tid];
-      store_out(dst + tid, v * (fast_exp2(refv - ref) / sum));
+      for (int e = 0; e < kVec; ++e)
+        for (int w = 1; w < kSplit; ++w) o[e] += s_acc[warp + w][lane * kVec + e];
     }
+    if (live)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) store_out(dst + lane * kVec + e, o[e] * inv);
     return;
   }
   // ---- weights ----
-  constexpr int kRowsEach = kCaChunk / kCaMergeThreads;
-  const int row0 = ((int)blockIdx.y - p.group) * kCaChunk;
-  if (row0 >= held) return;
+  constexpr int kRowsEach = 4, kRound = kRowsEach * kCaMergeThreads;
+  const int row0 = ((int)blockIdx.y - out_blocks) * kChunk, rows = min(held - row0, kChunk);
+  if (rows <= 0) return;
   const float* logits = p.logits + ((size_t)bh * p.c.cap + row0) * p.group;
-  float add[kRowsEach], first[kRowsEach][8];   // the weights, and the logits of the first eight heads
+  const size_t at = (size_t)bh * p.c.cap + row0;
+  float add[kRowsEach], first[kRowsEach][8];   // a round's weights, and its logits of the first eight heads
+  auto request = [&](int from) {
 #pragma unroll
-  for (int i = 0; i < kRowsEach; ++i) {
-    const int r = tid + i * kCaMergeThreads;
-    add[i] = row0 + r < held ? p.weights_in[(size_t)bh * p.c.cap + row0 + r] : 0.f;
-    if (p.group == 4) {
-      const float4 v = row0 + r < held ? reinterpret_cast<const float4*>(logits)[r] : make_float4(0.f, 0.f, 0.f, 0.f);
-      first[i][0] = v.x; first[i][1] = v.y; first[i][2] = v.z; first[i][3] = v.w;
-    } else {
+    for (int i = 0; i < kRowsEach; ++i) {
+      const int r = from + tid + i * kCaMergeThreads;
+      add[i] = r < rows ? p.weights_in[at + r] : 0.f;
+      if (p.group == 4) {
+        const float4 v = r < rows ? reinterpret_cast<const float4*>(logits)[r] : make_float4(0.f, 0.f, 0.f, 0.f);
+        first[i][0] = v.x; first[i][1] = v.y; first[i][2] = v.z; first[i][3] = v.w;
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) first[i][j] = j < p.group && row0 + r < held ? logits[(size_t)r * p.group + j] : 0.f;
+        for (int j = 0; j < 8; ++j) first[i][j] = j < p.group && r < rows ? logits[(size_t)r * p.group + j] : 0.f;
+      }
     }
-  }
-  for (int h0 = 0; h0 < p.group; h0 += 128) {
+  };
+  request(0);
+  for (int h0 = 0; h0 < p.group; h0 += 128) {   // 128 heads at a time; with more, the weights take several passes
     __syncthreads();
     for (int h = h0 + warp; h < min(p.group, h0 + 128); h += kWarps4) {
       const int pass = h / kCaHeads, pair = head * p.passes + pass;
@@ -644,25 +660,23 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
     }
     __syncthreads();
     const int n = min(p.group - h0, 128);
+    for (int from = 0; from < rows; from += kRound) {
+      if (from > 0 || h0 > 0) request(from);
 #pragma unroll
-    for (int i = 0; i < kRowsEach; ++i) {
-      const int r = tid + i * kCaMergeThreads;
-      if (row0 + r >= held) continue;
-      float sum = 0.f;
-      int j = 0;
-      if (h0 == 0) {
+      for (int i = 0; i < kRowsEach; ++i) {
+        const int r = from + tid + i * kCaMergeThreads;
+        if (r >= rows) continue;
+        float sum = 0.f;
+        int j = 0;
+        if (h0 == 0) {
 #pragma unroll
-        for (; j < 8; ++j)
-          if (j < n) sum += fast_exp2(first[i][j] - s_ref[j]) * s_inv[j];
+          for (; j < 8; ++j)
+            if (j < n) sum += fast_exp2(first[i][j] - s_ref[j]) * s_inv[j];
+        }
+        for (; j < n; ++j) sum += fast_exp2(logits[(size_t)r * p.group + h0 + j] - s_ref[j]) * s_inv[j];
+        p.weights_out[at + r] = (h0 ? p.weights_out[at + r] : add[i]) + sum;
       }
-      for (; j < n; ++j) sum += fast_exp2(logits[(size_t)r * p.group + h0 + j] - s_ref[j]) * s_inv[j];
-      add[i] += sum;
     }
-  }
-#pragma unroll
-  for (int i = 0; i < kRowsEach; ++i) {
-    const int r = tid + i * kCaMergeThreads;
-    if (row0 + r < held) p.weights_out[(size_t)bh * p.c.cap + row0 + r] = add[i];
   }
 }
 

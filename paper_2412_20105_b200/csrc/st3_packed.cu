@@ -354,6 +354,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
   using L = PkLayout<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
+  if (threadIdx.x == 0) { prefetch_map(&map_q); prefetch_map(&map_k); prefetch_map(&map_v); }
   if (!pk_begin<D, AttendRoles>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -661,6 +662,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
   using L = PkLayout<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
+  if (threadIdx.x == 0) { prefetch_map(&map_q); prefetch_map(&map_k); }
   if (!pk_begin<D, WeightRoles>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
