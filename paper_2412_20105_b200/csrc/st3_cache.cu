@@ -13,6 +13,8 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "st3_launch.cuh"
 
 namespace {
@@ -35,13 +37,25 @@ __device__ __forceinline__ int block_exp(float amax) {
   const int e = (int)(b >> 23) - 133 + ((b & 0x7fffffu) > 0x7e0000u);
   return min(max(e, -kMaxExp), kMaxExp);
 }
-__device__ __forceinline__ int code_of(float x, float inv_scale) {   // half to even
-  return (int)fminf(fmaxf(rintf(x * inv_scale), -127.f), 127.f);
+// Conversions between codes and floats without the conversion instructions, of which an SM has 16 a clock (two of them an element
+// bound the storing kernel at 22 of its 44 us for 24 000 rows of 8 heads).
+// x / scale rounded half to even, in the low byte: adding 1.5 * 2^23 leaves no bits below one.
+__device__ __forceinline__ unsigned code_bits(float x, float inv_scale) {
+  return __float_as_uint(fminf(fmaxf(x * inv_scale, -127.f), 127.f) + 12582912.f);
 }
-__device__ __forceinline__ unsigned pack4(int a, int b, int c, int d) {
-  return (unsigned)(a & 0xff) | ((unsigned)(b & 0xff) << 8) | ((unsigned)(c & 0xff) << 16) | ((unsigned)d << 24);
+__device__ __forceinline__ unsigned pack4(unsigned a, unsigned b, unsigned c, unsigned d) {   // the low bytes
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-__device__ __forceinline__ int byte_of(unsigned w, int i) { return (int)(signed char)(w >> (8 * i)); }
+// Code i of a word whose codes' sign bits have been inverted: 2^23 + 128 + code, less 2^23 + 128.
+__device__ __forceinline__ unsigned flip(unsigned w) { return w ^ 0x80808080u; }
+__device__ __forceinline__ float code_value(unsigned flipped, int i) {
+  return __uint_as_float(__byte_perm(flipped, 0x4b000000u, 0x7650 + i)) - 8388736.f;
+}
+// four codes times f, a power of two, rounded again
+__device__ __forceinline__ unsigned rescale4(unsigned w, float f) {
+  w = flip(w);
+  return pack4(code_bits(code_value(w, 0), f), code_bits(code_value(w, 1), f), code_bits(code_value(w, 2), f), code_bits(code_value(w, 3), f));
+}
 __device__ __forceinline__ int clamp_rows(int n, int cap) { return min(max(n, 0), cap); }
 
 struct CacheView {
@@ -79,9 +93,8 @@ __device__ __forceinline__ Raw8<T> load8(const T* p) {
   for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const uint4*>(p)[i];
   return r;
 }
-// the same as floats, with what is not finite as 0 (and noted in `bad`)
 template <typename T>
-__device__ __forceinline__ void values8(const Raw8<T>& r, float (&f)[8], bool& bad) {
+__device__ __forceinline__ void values8(const Raw8<T>& r, float (&f)[8]) {
   if constexpr (sizeof(T) == 2) {
     unpack16(r.w[0], f);
   } else {
@@ -89,10 +102,30 @@ __device__ __forceinline__ void values8(const Raw8<T>& r, float (&f)[8], bool& b
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (!(fabsf(f[i]) <= 3.4028235e38f)) { f[i] = 0.f; bad = true; }
 }
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+// the largest magnitude; NaN if one of them is
+template <typename T>
+__device__ __forceinline__ float top8(const Raw8<T>& r) {
+  if constexpr (sizeof(T) == 2) {
+    unsigned m = 0;
+    const unsigned u[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(u[i] & 0x7fff7fffu));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  } else {
+    float f[8], m = 0.f;
+    values8(r, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max_nan(m, fabsf(f[i]));
+    return m;
+  }
+}
+__device__ __forceinline__ float finite_or_0(float x) { return fabsf(x) <= 3.4028235e38f ? x : 0.f; }
 
 // The sequences' pieces are numbered so that no table is needed: sequence s has the numbers cu[s]/64 + 2 s and on, which are
 // at least as many as the blocks that its rows touch wherever they start (n/64 + 2).
@@ -100,24 +133,36 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const StoreParams p) {
   constexpr int kLanes = D / 8, kPass = kStoreThreads / kLanes, kIter = kBlockRows / kPass;
   __shared__ float s_max[2][kStoreThreads / 32];
+  __shared__ int s_seq, s_of[4];
   pdl_wait();
   pdl_next();
   const int tid = threadIdx.x, slot = blockIdx.x, head = blockIdx.y;
-  int below = 0;   // sequences whose first number is at most `slot`
-  for (int b0 = 0; b0 < p.c.batch; b0 += kStoreThreads) {
-    const int b = b0 + tid;
-    below += __syncthreads_count(b < p.c.batch && p.cu[min(b, p.c.batch - 1)] / kBlockRows + 2 * b <= slot);
+  // The sequence whose numbers hold `slot`, with its offsets: one round trip for all sequences.
+  if (tid == 0) s_seq = -1;
+  __syncthreads();
+  int found = -1, c0 = 0, c1 = 0, start = 0, pos = 0;
+  for (int b = tid; b < p.c.batch; b += kStoreThreads) {
+    const int from = p.cu[b], to = p.cu[b + 1], st = p.start ? p.start[b] : 0, ps = p.pos ? p.pos[b] : st;
+    if (from / kBlockRows + 2 * b <= slot && (b + 1 == p.c.batch || to / kBlockRows + 2 * (b + 1) > slot)) {
+      found = b; c0 = from; c1 = to; start = st; pos = ps;
+    }
   }
-  const int b = below - 1;
+  if (found >= 0) atomicMax(&s_seq, found);   // one, unless the offsets are not ascending
+  __syncthreads();
+  const int b = s_seq;
   if (b < 0) return;
-  const int c0 = p.cu[b], c1 = p.cu[b + 1], start = p.start ? p.start[b] : 0, pos = p.pos ? p.pos[b] : start;
+  if (b == found) { s_of[0] = c0; s_of[1] = c1; s_of[2] = start; s_of[3] = pos; }
+  __syncthreads();
+  c0 = s_of[0]; c1 = s_of[1]; start = s_of[2]; pos = s_of[3];
   const int n = c1 - c0;
   if (n == 0) return;
   if (n < 0 || c0 < 0 || c1 > p.total || start < 0 || start > p.c.cap - n) {   // reported, nothing stored
     if (tid == 0 && p.status) atomicOr(p.status, ST3_DEV_RANGE);
     return;
   }
-  const int blk = start / kBlockRows + (slot - (c0 / kBlockRows + 2 * b));
+  const int place = slot - (c0 / kBlockRows + 2 * b);
+  if (place < 0) return;
+  const int blk = start / kBlockRows + place;
   const int row0 = blk * kBlockRows;
   if (row0 >= start + n) return;
   const int lo = max(start - row0, 0), hi = min(start + n - row0, kBlockRows);   // new rows of this block
@@ -138,23 +183,37 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
 #pragma unroll
   for (int side = 0; side < 2; ++side) was[side] = lo > 0 ? p.c.scale[side][bh * (p.c.cap / kBlockRows) + blk] : 0.f;
   float amax[2] = {0.f, 0.f};
-  bool bad = false;
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
+  for (int side = 0; side < 2; ++side)
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
       const int r = r0 + i * kPass;
-      if (r >= lo && r < hi) {
-        float f[8];
-        values8(raw[side][i], f, bad);
+      if (r >= lo && r < hi) amax[side] = max_nan(amax[side], top8<T>(raw[side][i]));
+    }
+  // What is not finite counts as 0: rare, so that only blocks that hold some look at every element for it.
+  const bool bad = __syncthreads_or(!(amax[0] <= 3.4028235e38f && amax[1] <= 3.4028235e38f));
+  if (bad) {
+    if (tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax[side] = fmaxf(amax[side], fabsf(f[e]));
+    for (int side = 0; side < 2; ++side) {
+      amax[side] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kIter; ++i) {
+        const int r = r0 + i * kPass;
+        if (r < lo || r >= hi) continue;
+        float f[8];
+        values8<T>(raw[side][i], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax[side] = fmaxf(amax[side], fabsf(finite_or_0(f[e])));
       }
     }
+  }
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
     amax[side] = warp_max(amax[side]);
     if ((tid & 31) == 0) s_max[side][tid >> 5] = amax[side];
   }
-  if (__syncthreads_or(bad) && tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
+  __syncthreads();
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
 #pragma unroll
@@ -170,18 +229,19 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
       uint2* at = reinterpret_cast<uint2*>(codes + r * D + lane8);
       if (r >= lo && r < hi) {
         float f[8];
-        values8(raw[side][i], f, bad);
-        int c[8];
+        values8<T>(raw[side][i], f);
+        if (bad) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) c[j] = code_of(f[j], inv);
+          for (int j = 0; j < 8; ++j) f[j] = finite_or_0(f[j]);
+        }
+        unsigned c[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] = code_bits(f[j], inv);
         *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
       } else if (r < lo && e > e_was) {
         const uint2 w = *at;
         const float f = exp2i(max(e_was - e, -126));
-        int c[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) c[j] = code_of((float)byte_of(j < 4 ? w.x : w.y, j & 3), f);
-        *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+        *at = make_uint2(rescale4(w.x, f), rescale4(w.y, f));
       }
     }
     if (tid == 0) p.c.scale[side][bh * (p.c.cap / kBlockRows) + blk] = exp2i(e);
@@ -235,7 +295,7 @@ __global__ void __launch_bounds__(kRowsThreads) st3_cache_rows_kernel(const Rows
     const unsigned in[4] = {w.x, w.y, w.z, w.w};
     float f[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) f[j] = (float)byte_of(in[j >> 2], j & 3) * s;
+    for (int j = 0; j < 16; ++j) f[j] = code_value(flip(in[j >> 2]), j & 3) * s;
     T* out = dst + (bh * p.num_rows + i) * D + col;
     if constexpr (sizeof(T) == 2) {
       unsigned o[8];
@@ -288,25 +348,25 @@ __device__ __forceinline__ unsigned weight_key(float w, bool recent) {
   return min((b & 0x80000000u) ? ~b : b | 0x80000000u, 0xfffffffeu);
 }
 
-__device__ __forceinline__ int block_sum_below(int x, int* s_warp, int& total) {   // exclusive sum over the block
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int v = x;
+__device__ __forceinline__ int warp_sum_upto(int v) {   // inclusive
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int y = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += y;
   }
+  return v;
+}
+__device__ __forceinline__ int block_sum_below(int x, int* s_warp, int& total) {   // exclusive sum over the block
+  static_assert(kEvictThreads == 1024, "a lane for each warp's sum");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int v = warp_sum_upto(x);
   __syncthreads();
   if (lane == 31) s_warp[warp] = v;
   __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int i = 0; i < kEvictThreads / 32; ++i) {
-    const int y = s_warp[i];
-    all += y;
-    if (i < warp) before += y;
-  }
-  total = all;
+  const int sums = warp_sum_upto(s_warp[lane]);
+  total = __shfl_sync(0xffffffffu, sums, 31);
+  const int before = warp ? __shfl_sync(0xffffffffu, sums, warp - 1) : 0;
   return before + v - x;
 }
 
@@ -360,14 +420,10 @@ __global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const E
   if (tid == 0) {
     p.length[bh] = k;
     if (raw != n && p.status) atomicOr(p.status, ST3_DEV_RANGE);
-    if (k < p.from.cap) {
-      p.edge[2 * bh] = p.from.scale[0][(size_t)bh * blocks + k / kBlockRows];
-      p.edge[2 * bh + 1] = p.from.scale[1][(size_t)bh * blocks + k / kBlockRows];
-    }
   }
   for (int i = tid; i < blocks; i += kEvictThreads) p.changed[(size_t)bh * blocks + i] = 0;
   int* src = p.src + (size_t)bh * p.from.cap;
-  if (n <= p.keep) {
+  if (n <= p.keep) {   // no row comes from behind the new length: no scale is kept
     for (int i = tid; i < k; i += kEvictThreads) src[i] = i;
     return;
   }
@@ -399,18 +455,31 @@ __global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const E
   if (cutting.in_bin <= kEvictDirect) {
     if (tid == 0) { s_out[0] = 0; s_last = 0; }
     __syncthreads();
-    for (int i = tid; i < n; i += kEvictThreads) {
+    const int lane = tid & 31;
+    for (int i0 = 0; i0 < n; i0 += kEvictThreads) {
       int id;
-      const unsigned key = row_key(i, id);
-      if ((key >> 21) == cutting.bin) s_at_cut[atomicAdd(&s_out[0], 1)] = composite(key, id);
+      const unsigned key = i0 + tid < n ? row_key(i0 + tid, id) : 0u;
+      const bool yes = i0 + tid < n && (key >> 21) == cutting.bin;
+      const unsigned who = __ballot_sync(0xffffffffu, yes);
+      if (who) {
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&s_out[0], __popc(who));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1));
+        if (yes) s_at_cut[at] = composite(key, id);
+      }
     }
     __syncthreads();
-    if (tid < cutting.in_bin) {
-      const u64 mine = s_at_cut[tid];
+    // four lanes to a row, each against every fourth row
+    for (int c0 = 0; c0 < cutting.in_bin; c0 += kEvictThreads / 4) {
+      const int c = c0 + (tid >> 2);
+      const u64 mine = c < cutting.in_bin ? s_at_cut[c] : 0;
       int above = 0;
-#pragma unroll 8
-      for (int i = 0; i < cutting.in_bin; ++i) above += s_at_cut[i] > mine;
-      if (above == cutting.want - 1) s_last = mine;
+      if (c < cutting.in_bin)
+#pragma unroll 4
+        for (int i = tid & 3; i < cutting.in_bin; i += 4) above += s_at_cut[i] > mine;
+      above += __shfl_xor_sync(0xffffffffu, above, 1);
+      above += __shfl_xor_sync(0xffffffffu, above, 2);
+      if (c < cutting.in_bin && above == cutting.want - 1) s_last = mine;
     }
     __syncthreads();
     last = s_last;
@@ -464,6 +533,7 @@ __global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const E
     if (hole) p.changed[(size_t)bh * blocks + i / kBlockRows] = 1;
     base += total;
   }
+  if (tid < 2) p.edge[2 * bh + tid] = p.from.scale[tid][(size_t)bh * blocks + k / kBlockRows];   // k < n <= capacity
 }
 
 constexpr int kMoveThreads = 256;
@@ -518,10 +588,12 @@ __global__ void __launch_bounds__(kMoveThreads) st3_cache_move_kernel(const Evic
       const int r = (tid + i * kMoveThreads) / kLanes;
       if (r < rows) {
         const unsigned w[4] = {piece[side][i].x, piece[side][i].y, piece[side][i].z, piece[side][i].w};
-        int m = 0;
+        unsigned m = 0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) m = max(m, abs(byte_of(w[j >> 2], j & 3)));
-        amax[side] = fmaxf(amax[side], (float)m * s_scale[side][r]);
+        for (int j = 0; j < 4; ++j) m = __vmaxu4(m, __vabs4(w[j]));   // of -128, which no code is, 128
+        m = __vmaxu4(m, m >> 16);
+        m = max(m & 0xffu, (m >> 8) & 0xffu);
+        amax[side] = fmaxf(amax[side], __uint_as_float(0x4b000000u | m) * s_scale[side][r] - 8388608.f * s_scale[side][r]);
       }
     }
 #pragma unroll
@@ -546,12 +618,7 @@ __global__ void __launch_bounds__(kMoveThreads) st3_cache_move_kernel(const Evic
         uint4 o = piece[side][i];
         if (d) {
           const float f = exp2i(max(d, -126));
-          unsigned w[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = pack4(code_of((float)byte_of(w[j], 0), f), code_of((float)byte_of(w[j], 1), f),
-                         code_of((float)byte_of(w[j], 2), f), code_of((float)byte_of(w[j], 3), f));
-          o = make_uint4(w[0], w[1], w[2], w[3]);
+          o = make_uint4(rescale4(o.x, f), rescale4(o.y, f), rescale4(o.z, f), rescale4(o.w, f));
         }
         *reinterpret_cast<uint4*>(p.to.code[side] + ((size_t)bh * p.to.cap + row0 + r) * D + col) = o;
       }

@@ -55,7 +55,7 @@ struct CaLayout {
   static constexpr int kRed = kStages * kStage;              // sums of the four warps, 8 heads at a time
   static constexpr int kBars = kRed + kCaConsumers * 8 * kPitch * 4;
   static constexpr int kMl = kBars + 2 * kStages * 8;
-  static constexpr int kTotal = kMl + kCaConsumers * kCaHeads * 3 * 4 + 64;
+  static constexpr int kTotal = kMl + kCaConsumers * 8 * 3 * 4 + 64;
 };
 
 // The run of thread block c: blocks [total * c / grid, total * (c + 1) / grid), with grid <= total, so that none is empty.
@@ -140,7 +140,7 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
   uint64_t* empty = full + L::kStages;
   float* s_ml = reinterpret_cast<float*>(smem + L::kMl);
-  int* s_int = reinterpret_cast<int*>(s_ml + kCaConsumers * kCaHeads * 3);   // 16 ints
+  int* s_int = reinterpret_cast<int*>(s_ml + kCaConsumers * 8 * 3);   // 16 ints
   float* s_red = reinterpret_cast<float*>(smem + L::kRed);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -244,43 +244,58 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   int stage = 0;
   uint32_t parity = 0;
   bool ok = true;
-  while (x < x1) {
+  // A segment, and what it needs from memory, which is requested ahead of the end of the one before it.
+  struct Segment { int b, pair, h0, heads, i0, i1, held; size_t bh; } seg;
+  using Four = typename std::conditional<sizeof(T) == 2, uint2, float4>::type;
+  Four raw[kTiles][kSteps];   // queries: head g, dims 16 i + 4 t .. + 3
+  float ks32, vs32;           // the scales of 32 blocks, one a lane
+  auto request = [&] {
     int nb = blocks_of(p, b);
     while (x >= seq0 + nb * pairs) { seq0 += nb * pairs; nb = blocks_of(p, ++b); }
-    const int pair = (x - seq0) / nb, head = pair / p.passes, h0 = (pair - head * p.passes) * kCaHeads;
-    const int heads = min(p.group - h0, kCaHeads);   // of this pass
-    const int i0 = x - seq0 - pair * nb, i1 = min(nb, i0 + x1 - x);
-    const int held = clamp_rows(p.held[b], p.c.cap);
-    const size_t bh = (size_t)b * p.c.heads + head;
+    const int pair = (x - seq0) / nb, head = pair / p.passes;
+    seg.b = b;
+    seg.pair = pair;
+    seg.h0 = (pair - head * p.passes) * kCaHeads;
+    seg.heads = min(p.group - seg.h0, kCaHeads);   // of this pass
+    seg.i0 = x - seq0 - pair * nb;
+    seg.i1 = min(nb, seg.i0 + x1 - x);
+    seg.held = clamp_rows(p.held[b], p.c.cap);
+    seg.bh = (size_t)b * p.c.heads + head;
+    const size_t at = seg.bh * (p.c.cap / kBlockRows) + min(seg.i0 + lane, seg.i1 - 1);
+    ks32 = p.c.scale[0][at];
+    vs32 = p.c.scale[1][at];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      const bool live = n * 8 + g < seg.heads;
+      const T* src = static_cast<const T*>(p.q) + (seg.bh * p.group + seg.h0 + n * 8 + g) * D + 4 * t;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        raw[n][i] = Four{};
+        if (live) raw[n][i] = *reinterpret_cast<const Four*>(src + 16 * i);
+      }
+    }
+  };
+  request();
+  while (true) {
+    const Segment now = seg;
+    const int i0 = now.i0, i1 = now.i1, heads = now.heads, h0 = now.h0, held = now.held;
+    const size_t bh = now.bh;
     const float* ks = p.c.scale[0] + bh * (p.c.cap / kBlockRows);
     const float* vs = p.c.scale[1] + bh * (p.c.cap / kBlockRows);
-    float ks32, vs32;   // the scales of 32 blocks, one a lane; requested ahead of the queries
-    {
-      const int j = min(i0 + lane, i1 - 1);
-      ks32 = ks[j];
-      vs32 = vs[j];
-    }
-    // ---- the queries of this pass as B fragments: lane (g, t) holds head g, dims 16 i + 4 t .. + 3 ----
+    // ---- the queries of this pass as B fragments ----
     uint32_t qf[kTerms][kTiles][kSteps][2];
     float qs[kTiles][2];   // factor of the logits of heads 2 t and 2 t + 1
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      const int hq = n * 8 + g;
       float f[kSteps][4];
       float top = 0.f;
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        f[i][0] = f[i][1] = f[i][2] = f[i][3] = 0.f;
-        if (hq < heads) {
-          const T* src = static_cast<const T*>(p.q) + (((size_t)b * p.c.heads + head) * p.group + h0 + hq) * D + 16 * i + 4 * t;
-          if constexpr (sizeof(T) == 2) {
-            const uint2 w = *reinterpret_cast<const uint2*>(src);
-            f[i][0] = __uint_as_float(w.x << 16); f[i][1] = __uint_as_float(w.x & 0xffff0000u);
-            f[i][2] = __uint_as_float(w.y << 16); f[i][3] = __uint_as_float(w.y & 0xffff0000u);
-          } else {
-            const float4 w = *reinterpret_cast<const float4*>(src);
-            f[i][0] = w.x; f[i][1] = w.y; f[i][2] = w.z; f[i][3] = w.w;
-          }
+        if constexpr (sizeof(T) == 2) {
+          f[i][0] = __uint_as_float(raw[n][i].x << 16); f[i][1] = __uint_as_float(raw[n][i].x & 0xffff0000u);
+          f[i][2] = __uint_as_float(raw[n][i].y << 16); f[i][3] = __uint_as_float(raw[n][i].y & 0xffff0000u);
+        } else {
+          f[i][0] = raw[n][i].x; f[i][1] = raw[n][i].y; f[i][2] = raw[n][i].z; f[i][3] = raw[n][i].w;
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(f[i][e]));
@@ -440,68 +455,71 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       *fail = 1;
       if (lane == 0 && p.status) atomicOr(p.status, ST3_DEV_COPY_TIMEOUT);
     }
+    x += i1 - i0;
+    const bool more = x < x1;
+    // ahead of the sums where the registers allow it: a round trip under them
+    constexpr bool kEarly = sizeof(T) == 2 && kTiles == 1;
+    if (kEarly && ok && more) request();
 #pragma unroll
-    for (int n = 0; n < kTiles; ++n) {
+    for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l[n][j] += __shfl_xor_sync(0xffffffffu, l[n][j], o);
-        if (g == 0) {
-          float* dst = s_ml + (warp * kCaHeads + n * 8 + 2 * t + j) * 3;
-          dst[0] = m[n][j]; dst[1] = mv[n][j]; dst[2] = l[n][j];
-        }
-      }
-    }
-    if (ca_any_failed(!ok)) return;   // one verdict for the four warps: the barriers below count on all of them
-    const size_t slot = (size_t)blockIdx.x + (size_t)b * pairs + pair;
+    const size_t slot = (size_t)blockIdx.x + (size_t)now.b * pairs + now.pair;
     float* out_acc = p.part_acc + slot * p.pitch * D;
     float* out_ml = p.part_ml + slot * p.pitch * 3;
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      float f[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float all = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kCaConsumers; ++w) all = fmaxf(all, s_ml[(w * kCaHeads + n * 8 + 2 * t + j) * 3 + 1]);
-        f[j] = all > -INFINITY ? fast_exp2(mv[n][j] - all) : 0.f;
-      }
+      // One verdict for the four warps, as these barriers count on all of them; and nobody still reads what is overwritten here.
+      if (ca_any_failed(!ok)) return;
       float* dst = s_red + (size_t)warp * 8 * L::kPitch;
 #pragma unroll
       for (int c = 0; c < kSteps; ++c)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          *reinterpret_cast<float2*>(dst + (2 * t + j) * L::kPitch + 16 * c + 2 * g) = make_float2(acc[n][c][j] * f[j], acc[n][c][2 + j] * f[j]);
-      asm volatile("bar.sync 1, %0;" ::"n"(kCaConsumers * 32) : "memory");
-      for (int e = tid; e < 8 * D; e += kCaConsumers * 32) {
-        const int h = e / D, d = e - h * D;
-        if (n * 8 + h < heads) {
-          float sum = 0.f;
+          *reinterpret_cast<float2*>(dst + (2 * t + j) * L::kPitch + 16 * c + 2 * g) = make_float2(acc[n][c][j], acc[n][c][2 + j]);
+      if (g < 3) {   // lanes of three rows write one of the three numbers each
 #pragma unroll
-          for (int w = 0; w < kCaConsumers; ++w) sum += s_red[(w * 8 + h) * L::kPitch + d];
-          out_acc[(n * 8 + h) * D + d] = sum;
-        }
-      }
-      if (tid < 8 && n * 8 + tid < heads) {
-        float a = -INFINITY, av = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kCaConsumers; ++w) {
-          const float* src = s_ml + (w * kCaHeads + n * 8 + tid) * 3;
-          a = fmaxf(a, src[0]);
-          av = fmaxf(av, src[1]);
-        }
-        const float ref = a > -INFINITY ? a : 0.f;
-#pragma unroll
-        for (int w = 0; w < kCaConsumers; ++w) {
-          const float* src = s_ml + (w * kCaHeads + n * 8 + tid) * 3;
-          sum += src[2] * fast_exp2(src[0] - ref);
-        }
-        float* dst3 = out_ml + (n * 8 + tid) * 3;
-        dst3[0] = a; dst3[1] = av; dst3[2] = sum;
+        for (int j = 0; j < 2; ++j) s_ml[(warp * 8 + 2 * t + j) * 3 + g] = g == 0 ? m[n][j] : g == 1 ? mv[n][j] : l[n][j];
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kCaConsumers * 32) : "memory");
+      // 16 threads to a head
+      const int h = tid >> 4, d0 = (tid & 15) * 4;
+      float a[kCaConsumers], av[kCaConsumers], top = -INFINITY, topv = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kCaConsumers; ++w) {
+        a[w] = s_ml[(w * 8 + h) * 3];
+        av[w] = s_ml[(w * 8 + h) * 3 + 1];
+        top = fmaxf(top, a[w]);
+        topv = fmaxf(topv, av[w]);
+      }
+      const float ref = top > -INFINITY ? top : 0.f, refv = topv > -INFINITY ? topv : 0.f;
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kCaConsumers; ++w) {
+        sum += s_ml[(w * 8 + h) * 3 + 2] * fast_exp2(a[w] - ref);
+        av[w] = fast_exp2(av[w] - refv);
+      }
+      if (n * 8 + h < heads) {
+#pragma unroll
+        for (int d = 0; d < D; d += 64) {
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < kCaConsumers; ++w) {
+            const float4 v = *reinterpret_cast<const float4*>(s_red + (w * 8 + h) * L::kPitch + d0 + d);
+            o.x = fmaf(v.x, av[w], o.x); o.y = fmaf(v.y, av[w], o.y); o.z = fmaf(v.z, av[w], o.z); o.w = fmaf(v.w, av[w], o.w);
+          }
+          *reinterpret_cast<float4*>(out_acc + (n * 8 + h) * D + d0 + d) = o;
+        }
+        if (d0 == 0) {
+          float* dst3 = out_ml + (n * 8 + h) * 3;
+          dst3[0] = top; dst3[1] = topv; dst3[2] = sum;
+        }
+      }
     }
-    x += i1 - i0;
+    if (!more) break;
+    if (!kEarly) request();
   }
 }
 
