@@ -79,26 +79,40 @@ struct StoreParams {
   const int* pos;
   int* status;
   int total;
+  int wide;            // rows of both tensors start on 32 bytes
 };
 
 constexpr int kStoreThreads = 256;
 
-// 8 elements of a row as they come
+// 16 elements of a row as they come; `wide`: they start on 32 bytes
 template <typename T>
-struct Raw8 { uint4 w[sizeof(T) / 2]; };
+struct Raw16 { uint4 w[sizeof(T)]; };
 template <typename T>
-__device__ __forceinline__ Raw8<T> load8(const T* p) {
-  Raw8<T> r;
+__device__ __forceinline__ Raw16<T> load16(const T* p, bool wide) {
+  Raw16<T> r;
+  const uint4* q = reinterpret_cast<const uint4*>(p);
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const uint4*>(p)[i];
+  for (int i = 0; i < (int)sizeof(T); i += 2) {
+    if (wide) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w), "=r"(r.w[i + 1].x), "=r"(r.w[i + 1].y),
+                     "=r"(r.w[i + 1].z), "=r"(r.w[i + 1].w)
+                   : "l"(q + i));
+    } else {
+      r.w[i] = q[i];
+      r.w[i + 1] = q[i + 1];
+    }
+  }
   return r;
 }
+// eight of them as floats
 template <typename T>
-__device__ __forceinline__ void values8(const Raw8<T>& r, float (&f)[8]) {
+__device__ __forceinline__ void values8(const Raw16<T>& r, int half, float (&f)[8]) {
   if constexpr (sizeof(T) == 2) {
-    unpack16(r.w[0], f);
+    unpack16(r.w[half], f);
   } else {
-    const unsigned u[8] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w, r.w[1].x, r.w[1].y, r.w[1].z, r.w[1].w};
+    const uint4 a = r.w[2 * half], b = r.w[2 * half + 1];
+    const unsigned u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
   }
@@ -110,18 +124,25 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either 
 }
 // the largest magnitude; NaN if one of them is
 template <typename T>
-__device__ __forceinline__ float top8(const Raw8<T>& r) {
+__device__ __forceinline__ float top16(const Raw16<T>& r) {
   if constexpr (sizeof(T) == 2) {
     unsigned m = 0;
-    const unsigned u[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(u[i] & 0x7fff7fffu));
+    for (int h = 0; h < 2; ++h) {
+      const unsigned u[4] = {r.w[h].x, r.w[h].y, r.w[h].z, r.w[h].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(u[i] & 0x7fff7fffu));
+    }
     return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
   } else {
-    float f[8], m = 0.f;
-    values8(r, f);
+    float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max_nan(m, fabsf(f[i]));
+    for (int h = 0; h < 2; ++h) {
+      float f[8];
+      values8(r, h, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max_nan(m, fabsf(f[i]));
+    }
     return m;
   }
 }
@@ -131,7 +152,7 @@ __device__ __forceinline__ float finite_or_0(float x) { return fabsf(x) <= 3.402
 // at least as many as the blocks that its rows touch wherever they start (n/64 + 2).
 template <typename T, int D>
 __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const StoreParams p) {
-  constexpr int kLanes = D / 8, kPass = kStoreThreads / kLanes, kIter = kBlockRows / kPass;
+  constexpr int kLanes = D / 16, kPass = kStoreThreads / kLanes, kIter = kBlockRows / kPass;
   __shared__ float s_max[2][kStoreThreads / 32];
   __shared__ int s_seq, s_of[4];
   pdl_wait();
@@ -167,16 +188,16 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
   if (row0 >= start + n) return;
   const int lo = max(start - row0, 0), hi = min(start + n - row0, kBlockRows);   // new rows of this block
   const size_t bh = (size_t)b * p.c.heads + head;
-  const int lane8 = (tid % kLanes) * 8, r0 = tid / kLanes;
-  Raw8<T> raw[2][kIter];
+  const int col = (tid % kLanes) * 16, r0 = tid / kLanes;
+  Raw16<T> raw[2][kIter];
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
     const T* src = static_cast<const T*>(p.src[side]) + (long long)(c0 + row0 - start) * p.token_stride[side] +
-                   (long long)head * p.head_stride[side] + lane8;
+                   (long long)head * p.head_stride[side] + col;
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
       const int r = r0 + i * kPass;
-      if (r >= lo && r < hi) raw[side][i] = load8(src + (long long)r * p.token_stride[side]);
+      if (r >= lo && r < hi) raw[side][i] = load16(src + (long long)r * p.token_stride[side], p.wide);
     }
   }
   float was[2];   // read ahead of the barrier, written after it
@@ -188,7 +209,7 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
       const int r = r0 + i * kPass;
-      if (r >= lo && r < hi) amax[side] = max_nan(amax[side], top8<T>(raw[side][i]));
+      if (r >= lo && r < hi) amax[side] = max_nan(amax[side], top16(raw[side][i]));
     }
   // What is not finite counts as 0: rare, so that only blocks that hold some look at every element for it.
   const bool bad = __syncthreads_or(!(amax[0] <= 3.4028235e38f && amax[1] <= 3.4028235e38f));
@@ -201,10 +222,13 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
       for (int i = 0; i < kIter; ++i) {
         const int r = r0 + i * kPass;
         if (r < lo || r >= hi) continue;
-        float f[8];
-        values8<T>(raw[side][i], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax[side] = fmaxf(amax[side], fabsf(finite_or_0(f[e])));
+        for (int h = 0; h < 2; ++h) {
+          float f[8];
+          values8(raw[side][i], h, f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) amax[side] = fmaxf(amax[side], fabsf(finite_or_0(f[e])));
+        }
       }
     }
   }
@@ -226,22 +250,28 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
       const int r = r0 + i * kPass;
-      uint2* at = reinterpret_cast<uint2*>(codes + r * D + lane8);
+      uint4* at = reinterpret_cast<uint4*>(codes + r * D + col);
       if (r >= lo && r < hi) {
-        float f[8];
-        values8<T>(raw[side][i], f);
-        if (bad) {
+        unsigned w[4];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = finite_or_0(f[j]);
+        for (int h = 0; h < 2; ++h) {
+          float f[8];
+          values8(raw[side][i], h, f);
+          if (bad) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = finite_or_0(f[j]);
+          }
+          unsigned c[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) c[j] = code_bits(f[j], inv);
+          w[2 * h] = pack4(c[0], c[1], c[2], c[3]);
+          w[2 * h + 1] = pack4(c[4], c[5], c[6], c[7]);
         }
-        unsigned c[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) c[j] = code_bits(f[j], inv);
-        *at = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+        *at = make_uint4(w[0], w[1], w[2], w[3]);
       } else if (r < lo && e > e_was) {
-        const uint2 w = *at;
+        const uint4 w = *at;
         const float f = exp2i(max(e_was - e, -126));
-        *at = make_uint2(rescale4(w.x, f), rescale4(w.y, f));
+        *at = make_uint4(rescale4(w.x, f), rescale4(w.y, f), rescale4(w.z, f), rescale4(w.w, f));
       }
     }
     if (tid == 0) p.c.scale[side][bh * (p.c.cap / kBlockRows) + blk] = exp2i(e);
@@ -264,59 +294,66 @@ struct RowsParams {
   const int* first;
   const int* held;
   int num_rows;
+  int wide;            // the values' rows start on 32 bytes
 };
 
 constexpr int kRowsThreads = 256;
 
-// A thread reads 16 codes and writes 16 values; K and V are two halves of the grid's last dimension.
+// A thread reads 16 codes of a row and writes 16 values; K and V are two halves of the grid's last dimension.  (Two or four rows a
+// thread, or 8 codes, were slower by 10-15 %.)
 template <typename T, int D>
 __global__ void __launch_bounds__(kRowsThreads) st3_cache_rows_kernel(const RowsParams p) {
   constexpr int kLanes = D / 16, kPer = kRowsThreads / kLanes;
   pdl_wait();
   pdl_next();
-  const int side = blockIdx.z & 1, h = blockIdx.y, b = blockIdx.z >> 1;
-  const int i = blockIdx.x * kPer + threadIdx.x / kLanes;
+  const int side = blockIdx.z & 1, h = blockIdx.y, b = blockIdx.z >> 1, tid = threadIdx.x;
+  const int i0 = blockIdx.x * kPer, i = i0 + tid / kLanes;
   const int held = clamp_rows(p.held[b], p.c.cap);
-  const long long r = (long long)(p.first ? p.first[b] : 0) + i;
-  const bool live = r >= 0 && r < held;
+  const long long first = p.first ? p.first[b] : 0, r = first + i;
   const size_t bh = (size_t)b * p.c.heads + h;
   // selected, not indexed: an index would put the parameters into local memory
   T* dst = static_cast<T*>(side ? p.dst[1] : p.dst[0]);
   const int8_t* codes = side ? p.c.code[1] : p.c.code[0];
   const float* scales = side ? p.c.scale[1] : p.c.scale[0];
   if (i < p.num_rows && dst) {
-    const int col = (threadIdx.x % kLanes) * 16;
+    const int col = (tid % kLanes) * 16;
     uint4 w = make_uint4(0, 0, 0, 0);
     float s = 0.f;
-    if (live) {
+    if (r >= 0 && r < held) {
       w = *reinterpret_cast<const uint4*>(codes + (bh * p.c.cap + r) * D + col);
       s = scales[bh * (p.c.cap / kBlockRows) + r / kBlockRows];
     }
-    const unsigned in[4] = {w.x, w.y, w.z, w.w};
+    const unsigned in[4] = {flip(w.x), flip(w.y), flip(w.z), flip(w.w)};
     float f[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) f[j] = code_value(flip(in[j >> 2]), j & 3) * s;
+    for (int e = 0; e < 16; ++e) f[e] = code_value(in[e >> 2], e & 3) * s;
     T* out = dst + (bh * p.num_rows + i) * D + col;
     if constexpr (sizeof(T) == 2) {
       unsigned o[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const __nv_bfloat162 v2 = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
-        o[j] = *reinterpret_cast<const unsigned*>(&v2);
+      for (int e = 0; e < 8; ++e) {
+        const __nv_bfloat162 v2 = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+        o[e] = *reinterpret_cast<const unsigned*>(&v2);
       }
-      reinterpret_cast<uint4*>(out)[0] = make_uint4(o[0], o[1], o[2], o[3]);
-      reinterpret_cast<uint4*>(out)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      if (p.wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]),
+                     "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7])
+                     : "memory");
+      } else {
+        reinterpret_cast<uint4*>(out)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+        reinterpret_cast<uint4*>(out)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) reinterpret_cast<float4*>(out)[j] = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+      for (int e = 0; e < 4; ++e) reinterpret_cast<float4*>(out)[e] = make_float4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]);
     }
   }
-  const int i2 = blockIdx.x * kPer + threadIdx.x;   // ids and weights: the first threads of the K half
-  if (side == 0 && threadIdx.x < kPer && i2 < p.num_rows) {
-    const long long r2 = (long long)(p.first ? p.first[b] : 0) + i2;
-    const bool live2 = r2 >= 0 && r2 < held;
-    if (p.ids) p.ids[bh * p.num_rows + i2] = live2 ? p.c.ids[bh * p.c.cap + r2] : 0;
-    if (p.weights) p.weights[bh * p.num_rows + i2] = live2 ? p.c.weights[bh * p.c.cap + r2] : 0.f;
+  if (side == 0 && tid < kPer && i0 + tid < p.num_rows) {   // ids and weights: the K half
+    const long long r2 = first + i0 + tid;
+    const bool live = r2 >= 0 && r2 < held;
+    const size_t at = bh * p.num_rows + i0 + tid;
+    if (p.ids) p.ids[at] = live ? p.c.ids[bh * p.c.cap + r2] : 0;
+    if (p.weights) p.weights[at] = live ? p.c.weights[bh * p.c.cap + r2] : 0.f;
   }
 }
 
@@ -691,6 +728,8 @@ extern "C" st3_status st3_cache_store(const st3_cache* cache, const void* k, con
   p.token_stride[0] = k_token_stride; p.token_stride[1] = v_token_stride;
   p.head_stride[0] = k_head_stride; p.head_stride[1] = v_head_stride;
   p.cu = cu; p.start = start; p.pos = pos; p.status = dev_status; p.total = total;
+  p.wide = ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 31u) == 0 &&
+           ((k_token_stride | k_head_stride | v_token_stride | v_head_stride) & (2 * unit - 1)) == 0;
   const dim3 grid((unsigned)(total / kBlockRows + 2 * cache->batch), (unsigned)cache->num_kv_heads);
   const dim3 block(kStoreThreads);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
@@ -714,6 +753,7 @@ extern "C" st3_status st3_cache_rows(const st3_cache* cache, const int32_t* firs
   RowsParams p;
   p.c = view_of(cache);
   p.dst[0] = k; p.dst[1] = v; p.ids = ids; p.weights = weights; p.first = first; p.held = held; p.num_rows = num_rows;
+  p.wide = ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 31u) == 0;
   const int per = kRowsThreads / (cache->head_dim / 16);
   const dim3 grid((unsigned)((num_rows + per - 1) / per), (unsigned)cache->num_kv_heads, 2 * (unsigned)cache->batch);
   const dim3 block(kRowsThreads);
