@@ -374,7 +374,7 @@ struct EvictParams {
   int keep, recent, in_place;
 };
 
-constexpr int kEvictThreads = 1024;
+constexpr int kEvictThreads = 512;
 constexpr int kBins = 2048;
 
 // Weights as unsigned keys of the same order; -0 is 0, NaN the lowest, a recent row the highest.
@@ -395,13 +395,13 @@ __device__ __forceinline__ int warp_sum_upto(int v) {   // inclusive
   return v;
 }
 __device__ __forceinline__ int block_sum_below(int x, int* s_warp, int& total) {   // exclusive sum over the block
-  static_assert(kEvictThreads == 1024, "a lane for each warp's sum");
+  static_assert(kEvictThreads <= 1024, "a lane for each warp's sum");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int v = warp_sum_upto(x);
   __syncthreads();
   if (lane == 31) s_warp[warp] = v;
   __syncthreads();
-  const int sums = warp_sum_upto(s_warp[lane]);
+  const int sums = warp_sum_upto(lane < kEvictThreads / 32 ? s_warp[lane] : 0);
   total = __shfl_sync(0xffffffffu, sums, 31);
   const int before = warp ? __shfl_sync(0xffffffffu, sums, warp - 1) : 0;
   return before + v - x;
@@ -434,11 +434,12 @@ __device__ __forceinline__ Pick pick_bin(const int* s_hist, int bins, int want, 
 constexpr int kEvictStage = 8192;    // rows whose weight and position a block keeps in shared memory
 constexpr int kEvictDirect = 512;    // rows at the cut that are ranked one against the other
 constexpr int kEvictSmem = kEvictStage * 8;
+constexpr int kEvictAhead = 4;
 
 // Finds the last row that stays: by a histogram of the leading 11 bits of the weights' keys and, as its bin rarely holds many,
 // by ranking the rows in that bin directly, positions included; else by the remaining bits, 11 and 10 at a time, of keys and then of
 // positions.
-__global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const EvictParams p) {
+__global__ void __launch_bounds__(kEvictThreads, 2) st3_cache_select_kernel(const EvictParams p) {
   extern __shared__ __align__(16) unsigned char dyn[];
   unsigned* s_key = reinterpret_cast<unsigned*>(dyn);
   int* s_id = reinterpret_cast<int*>(dyn) + kEvictStage;
@@ -450,6 +451,17 @@ __global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const E
   pdl_wait();
   pdl_next();
   const int tid = threadIdx.x, bh = blockIdx.x, b = bh / p.from.heads;
+  const float* w = p.from.weights + (size_t)bh * p.from.cap;
+  const int* ids = p.from.ids + (size_t)bh * p.from.cap;
+  // the first rows travel with the count of them; what lies behind the count is not used
+  float w_ahead[kEvictAhead];
+  int id_ahead[kEvictAhead];
+#pragma unroll
+  for (int j = 0; j < kEvictAhead; ++j) {
+    const int i = tid + j * kEvictThreads;
+    w_ahead[j] = i < p.from.cap ? w[i] : 0.f;
+    id_ahead[j] = i < p.from.cap ? ids[i] : 0;
+  }
   const int raw = p.held[b];
   const int border = p.seen[b] - p.recent;   // the first position that counts as recent
   const int n = clamp_rows(raw, p.from.cap), k = min(n, p.keep);
@@ -464,22 +476,22 @@ __global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const E
     for (int i = tid; i < k; i += kEvictThreads) src[i] = i;
     return;
   }
-  const float* w = p.from.weights + (size_t)bh * p.from.cap;
-  const int* ids = p.from.ids + (size_t)bh * p.from.cap;
   const bool staged = n <= kEvictStage;
   bool nan = false;
   if (tid == 0) s_out[0] = 0;
   for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
   __syncthreads();
-#pragma unroll 4
-  for (int i = tid; i < n; i += kEvictThreads) {
-    const float wi = w[i];
-    const int id = ids[i];
+  auto take = [&](int i, float wi, int id) {
     nan |= wi != wi;
     const unsigned key = weight_key(wi, id >= border);
     if (staged) { s_key[i] = key; s_id[i] = id; }
     atomicAdd(&s_hist[key >> 21], 1);
-  }
+  };
+#pragma unroll
+  for (int j = 0; j < kEvictAhead; ++j)
+    if (tid + j * kEvictThreads < n) take(tid + j * kEvictThreads, w_ahead[j], id_ahead[j]);
+#pragma unroll 4
+  for (int i = tid + kEvictAhead * kEvictThreads; i < n; i += kEvictThreads) take(i, w[i], ids[i]);
   auto row_key = [&](int i, int& id) {
     id = staged ? s_id[i] : ids[i];
     return staged ? s_key[i] : weight_key(w[i], id >= border);
@@ -546,34 +558,74 @@ __global__ void __launch_bounds__(kEvictThreads) st3_cache_select_kernel(const E
     const unsigned key = row_key(i, id);
     return composite(key, id) >= last;
   };
-  // rows behind the new length that stay, in order
-  int* movers = p.movers + (size_t)bh * p.from.cap;
-  int base = 0;
-  for (int i0 = k; i0 < n; i0 += kEvictThreads) {
-    const int i = i0 + tid;
-    const int yes = i < n && stays(i);
+  if (staged) {
+    // a word of bits for 32 rows; one sum over the words numbers the holes (low half) and the rows that fill them (high half)
+    __shared__ unsigned s_word[kEvictStage / 32];
+    __shared__ int s_before[kEvictStage / 32];
+    const int words = (n + 31) / 32, lane = tid & 31;
+    for (int i0 = tid - lane; i0 < n; i0 += kEvictThreads) {
+      const unsigned bits = __ballot_sync(0xffffffffu, i0 + lane < n && stays(i0 + lane));
+      if (lane == 0) s_word[i0 / 32] = bits;
+    }
+    __syncthreads();
+    static_assert(kEvictStage / 32 <= kEvictThreads, "a thread for each word");
+    unsigned holes = 0, movers = 0;
+    auto split = [&](int word, unsigned& hole, unsigned& mover) {   // rows below k that go, rows from k on that stay
+      const int below = k - word * 32;
+      const unsigned mask = below >= 32 ? 0xffffffffu : below <= 0 ? 0u : (1u << below) - 1;
+      hole = ~s_word[word] & mask;
+      mover = s_word[word] & ~mask;
+    };
+    if (tid < words) split(tid, holes, movers);
     int total;
-    const int at = base + block_sum_below(yes, s_warp, total);
-    if (yes) movers[at] = i;
-    base += total;
-  }
-  __syncthreads();
-  const int moved = base;
-  base = 0;
-  for (int i0 = 0; i0 < k; i0 += kEvictThreads) {
-    const int i = i0 + tid;
-    const int hole = i < k && !stays(i);
-    int total;
-    const int at = base + block_sum_below(hole, s_warp, total);
-    // positions that are not distinct could leave a hole without a mover; it then keeps its row
-    if (i < k) src[i] = hole && at < moved ? movers[at] : i;
-    if (hole) p.changed[(size_t)bh * blocks + i / kBlockRows] = 1;
-    base += total;
+    const int before = block_sum_below(__popc(holes) | (__popc(movers) << 16), s_warp, total);
+    if (tid < words) {
+      s_before[tid] = before;
+      if (holes) p.changed[(size_t)bh * blocks + tid * 32 / kBlockRows] = 1;
+    }
+    __syncthreads();   // the keys have been read for the last time, too: the rows that move take their place
+    int* s_mover = reinterpret_cast<int*>(s_key);
+    for (int i = k / 32 * 32 + tid; i < n; i += kEvictThreads) {
+      split(i / 32, holes, movers);
+      if (movers >> (i & 31) & 1) s_mover[(s_before[i / 32] >> 16) + __popc(movers & ((1u << (i & 31)) - 1))] = i;
+    }
+    __syncthreads();
+    const int moved = total >> 16;
+    for (int i = tid; i < k; i += kEvictThreads) {
+      split(i / 32, holes, movers);
+      const int at = (s_before[i / 32] & 0xffff) + __popc(holes & ((1u << (i & 31)) - 1));
+      // positions that are not distinct could leave a hole without a row for it; it then keeps its own
+      src[i] = (holes >> (i & 31) & 1) && at < moved ? s_mover[at] : i;
+    }
+  } else {
+    // rows behind the new length that stay, in order
+    int* movers = p.movers + (size_t)bh * p.from.cap;
+    int base = 0;
+    for (int i0 = k; i0 < n; i0 += kEvictThreads) {
+      const int i = i0 + tid;
+      const int yes = i < n && stays(i);
+      int total;
+      const int at = base + block_sum_below(yes, s_warp, total);
+      if (yes) movers[at] = i;
+      base += total;
+    }
+    __syncthreads();
+    const int moved = base;
+    base = 0;
+    for (int i0 = 0; i0 < k; i0 += kEvictThreads) {
+      const int i = i0 + tid;
+      const int hole = i < k && !stays(i);
+      int total;
+      const int at = base + block_sum_below(hole, s_warp, total);
+      if (i < k) src[i] = hole && at < moved ? movers[at] : i;
+      if (hole) p.changed[(size_t)bh * blocks + i / kBlockRows] = 1;
+      base += total;
+    }
   }
   if (tid < 2) p.edge[2 * bh + tid] = p.from.scale[tid][(size_t)bh * blocks + k / kBlockRows];   // k < n <= capacity
 }
 
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 128;
 
 template <int D>
 __global__ void __launch_bounds__(kMoveThreads) st3_cache_move_kernel(const EvictParams p) {
