@@ -26,6 +26,12 @@ namespace {
 template <int kWarps>
 struct PkRoles {
   static constexpr int kMma = kWarps, kLoader = kWarps + 2, kThreads = (kWarps + 4) * 32;
+  // In the attention the control warps are the block's first ones, which the schedulers prefer: its MMAs are issued beside warps that
+  // always have something to issue (2 % at 12 000 tokens).  The weights lose 5 % that way.
+  static __device__ __forceinline__ int warp() {
+    const int w = threadIdx.x >> 5;
+    return kWarps == 16 ? w : w < 4 ? kWarps + w : w - 4;
+  }
   static constexpr int kRegsRows = kWarps == 8 ? 208 : 104, kRegsControl = kWarps == 8 ? 88 : 64;
   static_assert(kWarps == 8 || kWarps == 16, "2 * 208 + 88 = 3 * 168; 4 * 104 + 64 = 5 * 96");
 };
@@ -183,7 +189,7 @@ __device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int*
     mbar_fence_init();
   }
   __syncthreads();
-  if (threadIdx.x >> 5 == Roles::kMma) {
+  if (Roles::warp() == Roles::kMma) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(kPkTmem) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -198,7 +204,7 @@ template <typename Roles>
 __device__ __forceinline__ void pk_end(PkShared& sh, uint32_t tmem) {
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x >> 5 == Roles::kMma)
+  if (Roles::warp() == Roles::kMma)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kPkTmem) : "memory");
 }
 
@@ -318,12 +324,16 @@ __device__ __forceinline__ void pk_settle(PkShared& sh, int issued, int owned) {
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Causal attention.
-//   S = Q K^T (128 x 128, D/16 MMAs of K = 16), P = exp2(S - ref) as bf16 over the first half of its S, O += P V.
-// The tensor pipe runs PV_A(j) S_A(j+1) | PV_B(j) S_B(j+1) | ...: while one tile's softmax runs, the other tile's two
-// products do.  P goes back in two halves of 64 keys, the first of which P V starts on while the second is computed.  `ref`
-// follows a row's maximum only when that has grown by 2^64: bf16 and fp32 have the range for it and lose no bits, and
-// O is then hardly ever rescaled.  S(j) complete says that P V(j-1) is, which came before it in the pipe.
+// Causal attention, in steps of 64 keys, two to a tile that comes through the ring.
+//   S = Q K^T (128 x 64, D/16 MMAs of K = 16), P = exp2(S - ref) as bf16 over the first half of its S, O += P V.
+// The tensor pipe runs S(0) S(1) | PV(0) S(2) | PV(1) S(3) | ... for each tile, so that the softmax of a step runs under the products
+// of the one before it and of the other tile.  `ref` follows a row's maximum only when that has grown by 2^64: bf16 and
+// fp32 have the range for it and lose no bits, and O is then hardly ever rescaled.
+// What bounds it at long prompts: the MMAs, of which a 128x128x16 takes 64 cycles but a 128x64x16 49, as long as its operands take to
+// read from shared memory: 2 600 cycles for both tiles and 128 keys at D = 128, of 3 200 measured (12 000 and 3 043 tokens, 32 heads
+// of 128: 0.97 ms alone, 1 290 TFLOP/s).  Scores of 128 keys would cost 64 cycles an MMA but leave tensor memory no second
+// buffer: a tile's softmax and products then form one chain (3 850 cycles).  At short ones (98 us for 16 prompts of 690 tokens) it
+// is the start and the end of an item, some 6 000 cycles of its 17 000.
 // ------------------------------------------------------------------------------------------------------------------
 // exp2(s * sc - ref) of a step's columns, as bf16 pairs in w and added up in `add`.  Whole steps take every fourth pair on the
 // FMA pipe; where columns are masked (-Inf, which have to give 0) the special-function unit does them all.
@@ -357,7 +367,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
   if (threadIdx.x == 0) { prefetch_map(&map_q); prefetch_map(&map_k); prefetch_map(&map_v); }
   if (!pk_begin<D, AttendRoles>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int lane = threadIdx.x & 31, warp = AttendRoles::warp();
   volatile int* fail = &sh.fail;
   const int rows = p.by_heads ? kPkRows : 2 * kPkRows;
   if (warp >= AttendRoles::kMma) pk_fewer_registers<AttendRoles>();
@@ -625,6 +635,8 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 //   S^T = K Q^T with the keys as rows: a thread owns a key and adds up its row, so nothing is exchanged and no sum's order
 // changes.  Tensor memory holds two S^T for each of the two key tiles; a product runs while the one before it is read.
 // Queries that do not count (before the window, behind the sequence) are left out of the sums.
+// What bounds it: the exponentials, of which the special-function unit does 16 a clock and the FMA pipe takes a quarter: 1 540
+// cycles for both tiles and 128 queries, of 3 000 measured (85 us for 16 prompts of 690 tokens); the MMAs take 1 030.
 // ------------------------------------------------------------------------------------------------------------------
 // Adds exp2(s * sc - lse) of 32 queries; kSome: of those in [lo, hi) only, whatever the others are.
 template <bool kSome>
@@ -665,7 +677,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
   if (threadIdx.x == 0) { prefetch_map(&map_q); prefetch_map(&map_k); }
   if (!pk_begin<D, WeightRoles>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int lane = threadIdx.x & 31, warp = WeightRoles::warp();
   volatile int* fail = &sh.fail;
   const int rows = 2 * kPkRows;
 
