@@ -322,7 +322,7 @@ def _stream_of(index: int) -> int:
 
 def _dense(t, shape, dtype, index, what):
     """Address of a dense tensor on CUDA device `index`."""
-    if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.is_cuda and t.get_device() == index:
+    if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == index:
         return t.data_ptr()
     raise ValueError(f"{what}: a contiguous {dtype} tensor of {tuple(shape)} on cuda:{index} is needed, "
                      f"not {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -330,53 +330,65 @@ def _dense(t, shape, dtype, index, what):
 
 def _rows_view(t, heads, dim, dtype, index, what):
     """Address and (token, head) strides of a [tokens, heads, dim] tensor whose last dimension is dense."""
-    if t.dim() != 3 or t.size(1) != heads or t.size(2) != dim or t.dtype is not dtype or not t.is_cuda or t.get_device() != index:
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or t.dtype is not dtype or t.get_device() != index:
         raise ValueError(f"{what}: a {dtype} tensor of [tokens, {heads}, {dim}] on cuda:{index} is needed, "
-                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+                         f"not {t.dtype} {tuple(shape)} on {t.device}")
     token, head, one = t.stride()
     if one != 1:
         raise ValueError(f"{what}: the elements of a head have to lie side by side")
-    return t.data_ptr(), (token, head)
+    return t.data_ptr(), token, head
 
 
-def _packed(q, k, cu):
-    import torch
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q and k: tensors of [tokens, heads, dim] are needed")
+def _packed_shape(q, k):
+    """(total, heads, kv heads, dim, device index) of packed queries and keys."""
+    if q.dim() != 3 or k.dim() != 3 or not q.is_cuda:
+        raise ValueError("q and k: CUDA tensors of [tokens, heads, dim] are needed")
     total, heads, dim = q.shape
-    qp, qs = _rows_view(q, heads, dim, q.dtype, q.get_device(), "q")
-    kp, ks = _rows_view(k, k.shape[1], dim, q.dtype, q.get_device(), "k")
     if k.shape[0] != total:
         raise ValueError("q and k have different numbers of tokens")
+    return total, heads, k.shape[1], dim, q.get_device()
+
+
+def _starts_of(cu, index):
+    import torch
     if cu.dim() != 1 or cu.numel() < 1:
         raise ValueError("cu: [sequences + 1] is needed")
-    desc = PackedDesc(cu.numel() - 1, total, heads, k.shape[1], dim, _dtype_of(q), *qs, *ks, *ks, *qs)
-    return desc, qp, kp, _dense(cu, cu.shape, torch.int32, q.get_device(), "cu")
+    return _dense(cu, cu.shape, torch.int32, index, "cu")
 
 
 def packed_attend(q, k, v, cu, out, lse=None, status=None):
     """Causal attention of packed prompts: q, out [tokens, heads, dim], k, v [tokens, kv heads, dim], lse [heads, tokens]."""
     import torch
-    desc, qp, kp, cup = _packed(q, k, cu)
-    vp, (desc.v_token_stride, desc.v_head_stride) = _rows_view(v, k.shape[1], q.shape[2], q.dtype, q.get_device(), "v")
-    op, (desc.out_token_stride, desc.out_head_stride) = _rows_view(out, q.shape[1], q.shape[2], q.dtype, q.get_device(), "out")
-    if v.shape[0] != q.shape[0] or out.shape[0] != q.shape[0]:
+    total, heads, kv, dim, index = _packed_shape(q, k)
+    dtype = q.dtype
+    qp, *qs = _rows_view(q, heads, dim, dtype, index, "q")
+    kp, *ks = _rows_view(k, kv, dim, dtype, index, "k")
+    vp, *vs = _rows_view(v, kv, dim, dtype, index, "v")
+    op, *os_ = _rows_view(out, heads, dim, dtype, index, "out")
+    if v.shape[0] != total or out.shape[0] != total:
         raise ValueError("q, v and out have different numbers of tokens")
+    cup = _starts_of(cu, index)
+    desc = PackedDesc(cu.numel() - 1, total, heads, kv, dim, _dtype_of(q), *qs, *ks, *vs, *os_)
     st3_packed_attend(desc, qp, kp, vp, cup, op,
-                      None if lse is None else _dense(lse, (q.shape[1], q.shape[0]), torch.float32, q.get_device(), "lse"),
-                      None if status is None else _dense(status, (1,), torch.int32, q.get_device(), "status"), _stream_of(q.get_device()))
+                      None if lse is None else _dense(lse, (heads, total), torch.float32, index, "lse"),
+                      None if status is None else _dense(status, (1,), torch.int32, index, "status"), _stream_of(index))
 
 
 def packed_weights(q, k, lse, cu, weights, window=0, status=None):
     """What each token has received from all queries, or from the last `window`: weights [sequences, kv heads, capacity]."""
     import torch
-    desc, qp, kp, cup = _packed(q, k, cu)
+    total, heads, kv, dim, index = _packed_shape(q, k)
+    qp, *qs = _rows_view(q, heads, dim, q.dtype, index, "q")
+    kp, *ks = _rows_view(k, kv, dim, q.dtype, index, "k")
+    cup = _starts_of(cu, index)
     if weights.dim() != 3:
         raise ValueError("weights: [sequences, kv heads, capacity] is needed")
-    shape = (desc.num_seqs, desc.num_kv_heads, weights.shape[2])
-    st3_packed_weights(desc, qp, kp, _dense(lse, (q.shape[1], q.shape[0]), torch.float32, q.get_device(), "lse"), cup,
-                       _dense(weights, shape, torch.float32, q.get_device(), "weights"), weights.shape[2], window,
-                       None if status is None else _dense(status, (1,), torch.int32, q.get_device(), "status"), _stream_of(q.get_device()))
+    seqs, capacity = cu.numel() - 1, weights.shape[2]
+    desc = PackedDesc(seqs, total, heads, kv, dim, _dtype_of(q), *qs, *ks, *ks, *qs)
+    st3_packed_weights(desc, qp, kp, _dense(lse, (heads, total), torch.float32, index, "lse"), cup,
+                       _dense(weights, (seqs, kv, capacity), torch.float32, index, "weights"), capacity, window,
+                       None if status is None else _dense(status, (1,), torch.int32, index, "status"), _stream_of(index))
 
 
 class Cache:
@@ -428,8 +440,8 @@ class Cache:
     def store(self, k, v, cu, start=None, pos=None):
         """Rows cu[s] .. cu[s+1]-1 of k and v ([tokens, kv heads, dim]) go behind the start[s] rows of sequence s."""
         dt = _dtype_of(k)
-        kp, ks = _rows_view(k, self.num_kv_heads, self.head_dim, k.dtype, self._index, "k")
-        vp, vs = _rows_view(v, self.num_kv_heads, self.head_dim, k.dtype, self._index, "v")
+        kp, *ks = _rows_view(k, self.num_kv_heads, self.head_dim, k.dtype, self._index, "k")
+        vp, *vs = _rows_view(v, self.num_kv_heads, self.head_dim, k.dtype, self._index, "v")
         if v.shape[0] != k.shape[0]:
             raise ValueError("k and v have different numbers of rows")
         st3_cache_store(self.desc, kp, vp, dt, ks, vs, _dense(cu, (self.batch + 1,), self.torch.int32, self._index, "cu"),
