@@ -76,7 +76,7 @@ struct PkItem {
 
 struct PkShared {
   uint64_t full[8], empty[8];           // ring of the other operand
-  uint64_t own, own_free;               // the item's own two tiles
+  uint64_t own[2], own_free[2];         // the item's own two tiles (weights: two buffers of them)
   uint64_t scores[4];                   // S is complete (two buffers a tile)
   uint64_t taken[4];                    // attention: P is in tensor memory; weights: S has been read
   uint64_t added[2], done[2];           // attention: a P V, and the last one of an item, is complete
@@ -88,18 +88,20 @@ struct PkShared {
   int fail;
 };
 
-template <int D>
+// kBuffers: of an item's own tiles.  Two in the weights, whose items can be as short as one step a head: the next one's keys come
+// while this one's are used.  The attention's own tiles come while its outputs are written.
+template <int D, int kBuffers>
 struct PkLayout {
   static constexpr int kBoxes = D / 64;
   static constexpr int kTile = kBoxes * kBox;
-  static constexpr int kStages = D == 128 ? 5 : 8;
-  static constexpr int kRing = 2 * kTile;
+  static constexpr int kStages = D == 128 ? 7 - 2 * kBuffers : 8;
+  static constexpr int kRing = 2 * kBuffers * kTile;
   static constexpr int kShared = kRing + kStages * kTile;
-  static constexpr int kLse = kShared + 768;                       // weights: two buffers of 64 sums for each warpgroup
-  static constexpr int kTotal = kShared + 768, kTotalWeights = kLse + 4 * 2 * 64 * 4;
+  static constexpr int kLse = kShared + 768;   // weights: two buffers of 64 sums for each of the four warpgroups
+  static constexpr int kTotal = kLse + (kBuffers == 2 ? 4 * 2 * 64 * 4 : 0);
 };
 static_assert(sizeof(PkShared) <= 768, "PkShared must fit its slot");
-static_assert(PkLayout<128>::kTotalWeights <= 227 * 1024, "shared memory");
+static_assert(PkLayout<128, 2>::kTotal <= 227 * 1024 && PkLayout<128, 1>::kTotal <= 227 * 1024, "shared memory");
 
 // Bounded wait that also ends when another role of the block has given up.
 __device__ __forceinline__ bool pk_wait(uint64_t* bar, uint32_t parity, volatile int* fail) {
@@ -134,10 +136,10 @@ __device__ __forceinline__ int taken_index(const void* answer) {
   return got ? (int)x : -1;
 }
 
-template <int D>
+template <int kBoxes>
 __device__ __forceinline__ void load_tile(unsigned char* dst, const CUtensorMap* map, int head, int row, uint64_t* bar) {
 #pragma unroll
-  for (int x = 0; x < PkLayout<D>::kBoxes; ++x) tma_load_3d(dst + x * kBox, map, x * 64, head, row, bar);
+  for (int x = 0; x < kBoxes; ++x) tma_load_3d(dst + x * kBox, map, x * 64, head, row, bar);
 }
 
 // The sequence of number `slot` (`rows` tokens a number): how many sequences start at or below it, less one.  A whole warp.
@@ -172,7 +174,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 }
 
 // The barriers, the tensor memory and the start of a block; false if its shared memory is not where it must be.
-template <int D, typename Roles>
+template <int kStages, typename Roles>
 __device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int* status) {
   if (smem_u32(smem) & 1023u) {   // the swizzle assumes aligned tiles: reported, not used
     if (threadIdx.x == 0 && status) atomicOr(status, ST3_DEV_RANGE);
@@ -180,9 +182,8 @@ __device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int*
     return false;
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < PkLayout<D>::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 2); }
-    mbar_init(&sh.own, 1);
-    mbar_init(&sh.own_free, 2);
+    for (int i = 0; i < kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 2); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.own[i], 1); mbar_init(&sh.own_free[i], 2); }
     for (int i = 0; i < 4; ++i) { mbar_init(&sh.scores[i], 1); mbar_init(&sh.taken[i], Roles::kMma / 2); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.added[i], 1); mbar_init(&sh.done[i], 1); mbar_init(&sh.ready[i], 1); mbar_init(&sh.read[i], Roles::kMma + 2); }
     mbar_init(&sh.next, 1);
@@ -317,11 +318,11 @@ struct Ring {
   __device__ __forceinline__ void step() { if (++stage == kStages) { stage = 0; phase ^= 1; } }
 };
 
-// Copies still in flight when the loader leaves: the last use of every stage, and the item's own tiles.
-template <int kStages>
+// Copies still in flight when the loader leaves: the last use of every stage, and of the buffers of an item's own tiles.
+template <int kStages, int kBuffers>
 __device__ __forceinline__ void pk_settle(PkShared& sh, int issued, int owned) {
   for (int u = max(0, issued - kStages); u < issued; ++u) pf_wait(&sh.full[u % kStages], (u / kStages) & 1);
-  if (owned > 0) pf_wait(&sh.own, (owned - 1) & 1);
+  for (int u = max(0, owned - kBuffers); u < owned; ++u) pf_wait(&sh.own[u % kBuffers], (u / kBuffers) & 1);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -362,11 +363,11 @@ template <int D>
 __global__ void __launch_bounds__(AttendRoles::kThreads, 1)
 st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                          const __grid_constant__ CUtensorMap map_v, const PackedParams p) {
-  using L = PkLayout<D>;
+  using L = PkLayout<D, 1>;
   extern __shared__ __align__(1024) unsigned char smem[];
   PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
   if (threadIdx.x == 0) { prefetch_map(&map_q); prefetch_map(&map_k); prefetch_map(&map_v); }
-  if (!pk_begin<D, AttendRoles>(smem, sh, p.status)) return;
+  if (!pk_begin<L::kStages, AttendRoles>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
   const int lane = threadIdx.x & 31, warp = AttendRoles::warp();
   volatile int* fail = &sh.fail;
@@ -398,12 +399,12 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
           return true;
         },
         [&](const PkItem& it) {
-          bool ok = pk_wait_warp(&sh.own_free, (owned & 1) ^ 1, fail);
+          bool ok = pk_wait_warp(&sh.own_free[0], (owned & 1) ^ 1, fail);
           if (!ok) return false;
           if (lane == 0) {
-            mbar_expect_tx(&sh.own, 2 * L::kTile);
+            mbar_expect_tx(&sh.own[0], 2 * L::kTile);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) load_tile<D>(smem + x * L::kTile, &map_q, it.head[x], it.row + it.first[x], &sh.own);
+            for (int x = 0; x < 2; ++x) load_tile<L::kBoxes>(smem + x * L::kTile, &map_q, it.head[x], it.row + it.first[x], &sh.own[0]);
           }
           ++owned;
           const int n = max(it.steps[0], it.steps[1]), kv = it.head[0] / p.group;
@@ -412,7 +413,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             if (!ok) break;
             if (lane == 0) {
               mbar_expect_tx(&sh.full[ring.stage], L::kTile);
-              load_tile<D>(smem + L::kRing + ring.stage * L::kTile, j & 1 ? &map_v : &map_k, kv, it.row + (j >> 1) * kPkRows, &sh.full[ring.stage]);
+              load_tile<L::kBoxes>(smem + L::kRing + ring.stage * L::kTile, j & 1 ? &map_v : &map_k, kv, it.row + (j >> 1) * kPkRows, &sh.full[ring.stage]);
             }
             __syncwarp();
             ++issued;
@@ -420,7 +421,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
           }
           return ok;
         });
-    if (lane == 0) pk_settle<L::kStages>(sh, issued, owned);
+    if (lane == 0) pk_settle<L::kStages, 1>(sh, issued, owned);
     __syncwarp();
   } else if (warp >= AttendRoles::kMma) {
     // ===================== MMA: a warp for each tile =====================
@@ -436,7 +437,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     bool ok = true;
     while (ok && pk_item(sh, slot, phase, it)) {
       const int mine = uniform(2 * (x ? it.steps[1] : it.steps[0])), n = uniform(max(it.steps[0], it.steps[1])), len = uniform(it.len);
-      ok = pk_wait_warp(&sh.own, own, fail);
+      ok = pk_wait_warp(&sh.own[0], own, fail);
       own ^= 1;
       // S = Q K^T of the two steps of a tile of keys at the ring's place, which is then left
       Ring<L::kStages> k;
@@ -456,7 +457,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         if (t & 1) {
           if (elected()) {
             umma_commit(&sh.empty[k.stage]);
-            if (t == 2 * n - 1) umma_commit(&sh.own_free);
+            if (t == 2 * n - 1) umma_commit(&sh.own_free[0]);
           }
           __syncwarp();
         }
@@ -672,11 +673,11 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[64], int part, c
 template <int D>
 __global__ void __launch_bounds__(WeightRoles::kThreads, 1)
 st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const PackedParams p) {
-  using L = PkLayout<D>;
+  using L = PkLayout<D, 2>;
   extern __shared__ __align__(1024) unsigned char smem[];
   PkShared& sh = *reinterpret_cast<PkShared*>(smem + L::kShared);
   if (threadIdx.x == 0) { prefetch_map(&map_q); prefetch_map(&map_k); }
-  if (!pk_begin<D, WeightRoles>(smem, sh, p.status)) return;
+  if (!pk_begin<L::kStages, WeightRoles>(smem, sh, p.status)) return;
   const uint32_t tmem = sh.tmem;
   const int lane = threadIdx.x & 31, warp = WeightRoles::warp();
   volatile int* fail = &sh.fail;
@@ -717,12 +718,13 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
           return true;
         },
         [&](const PkItem& it) {
-          bool ok = pk_wait_warp(&sh.own_free, (owned & 1) ^ 1, fail);
+          const int buf = owned & 1;
+          bool ok = pk_wait_warp(&sh.own_free[buf], ((owned >> 1) & 1) ^ 1, fail);
           if (!ok) return false;
           if (lane == 0) {
-            mbar_expect_tx(&sh.own, 2 * L::kTile);
+            mbar_expect_tx(&sh.own[buf], 2 * L::kTile);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) load_tile<D>(smem + x * L::kTile, &map_k, it.head[x], it.row + it.first[x], &sh.own);
+            for (int x = 0; x < 2; ++x) load_tile<L::kBoxes>(smem + (2 * buf + x) * L::kTile, &map_k, it.head[x], it.row + it.first[x], &sh.own[buf]);
           }
           ++owned;
           const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
@@ -732,7 +734,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
               if (!ok) break;
               if (lane == 0) {
                 mbar_expect_tx(&sh.full[ring.stage], L::kTile);
-                load_tile<D>(smem + L::kRing + ring.stage * L::kTile, &map_q, it.head[0] * p.group + g, it.row + it.begin + t * kPkRows, &sh.full[ring.stage]);
+                load_tile<L::kBoxes>(smem + L::kRing + ring.stage * L::kTile, &map_q, it.head[0] * p.group + g, it.row + it.begin + t * kPkRows, &sh.full[ring.stage]);
               }
               __syncwarp();
               ++issued;
@@ -740,20 +742,21 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             }
           return ok;
         });
-    if (lane == 0) pk_settle<L::kStages>(sh, issued, owned);
+    if (lane == 0) pk_settle<L::kStages, 2>(sh, issued, owned);
     __syncwarp();
   } else if (warp >= WeightRoles::kMma) {
     const int x = warp - WeightRoles::kMma;   // a warp for each tile
     const uint32_t own_lo = uniform(desc_lo(smem_u32(smem + x * L::kTile), 16)), ring_lo = uniform(desc_lo(smem_u32(smem + L::kRing), 16));
     Ring<L::kStages> ring;
     int slot = 0;
-    uint32_t phase = 0, own = 0, use = 0;   // use: S^T buffers used so far
+    uint32_t phase = 0, owned = 0, use = 0;   // owned: items so far; use: S^T buffers used so far
     PkItem it;
     bool ok = true;
     while (ok && pk_item(sh, slot, phase, it)) {
       const int tiles = uniform((it.len - it.begin + kPkRows - 1) / kPkRows), mine = uniform(x ? it.steps[1] : it.steps[0]);
-      ok = pk_wait_warp(&sh.own, own, fail);
-      own ^= 1;
+      const uint32_t own_buf = owned & 1, mine_lo = uniform(own_lo + own_buf * (2 * L::kTile >> 4));
+      ok = pk_wait_warp(&sh.own[own_buf], (owned >> 1) & 1, fail);
+      ++owned;
       for (int t = uniform(it.steps[0]); t < tiles && ok; ++t)
         for (int g = 0; g < p.group && ok; ++g) {
           ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
@@ -772,12 +775,12 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 #pragma unroll
               for (int ks = 0; ks < D / 16; ++ks) {
                 const uint32_t off = ((ks >> 2) * kBox + (ks & 3) * 32) >> 4;
-                umma_bf16(tS, own_lo + off, q_lo + off, kIdescScores, ks > 0);
+                umma_bf16(tS, mine_lo + off, q_lo + off, kIdescScores, ks > 0);
               }
               umma_commit(&sh.scores[bar]);
             }
             umma_commit(&sh.empty[ring.stage]);
-            if (t == tiles - 1 && g == p.group - 1) umma_commit(&sh.own_free);
+            if (t == tiles - 1 && g == p.group - 1) umma_commit(&sh.own_free[own_buf]);
           }
           __syncwarp();
           ring.step();
@@ -897,13 +900,13 @@ PackedParams packed_params(const st3_packed* p, const int32_t* cu, int* status) 
 
 template <int D>
 st3_status attend_launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const PackedParams& d, cudaStream_t s) {
-  if (!allow_smem<st3_packed_attend_kernel<D>>(PkLayout<D>::kTotal)) return ST3_ERR_CUDA;
-  return launch(st3_packed_attend_kernel<D>, dim3((unsigned)d.items), dim3(AttendRoles::kThreads), PkLayout<D>::kTotal, s, mq, mk, mv, d);
+  if (!allow_smem<st3_packed_attend_kernel<D>>(PkLayout<D, 1>::kTotal)) return ST3_ERR_CUDA;
+  return launch(st3_packed_attend_kernel<D>, dim3((unsigned)d.items), dim3(AttendRoles::kThreads), PkLayout<D, 1>::kTotal, s, mq, mk, mv, d);
 }
 template <int D>
 st3_status weights_launch(const CUtensorMap& mq, const CUtensorMap& mk, const PackedParams& d, cudaStream_t s) {
-  if (!allow_smem<st3_packed_weights_kernel<D>>(PkLayout<D>::kTotalWeights)) return ST3_ERR_CUDA;
-  return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(WeightRoles::kThreads), PkLayout<D>::kTotalWeights, s, mq, mk, d);
+  if (!allow_smem<st3_packed_weights_kernel<D>>(PkLayout<D, 2>::kTotal)) return ST3_ERR_CUDA;
+  return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(WeightRoles::kThreads), PkLayout<D, 2>::kTotal, s, mq, mk, d);
 }
 
 }  // namespace
