@@ -887,7 +887,7 @@ AttendLayout attend_layout(const st3_cache* c, int heads, bool weights) {
   l.group = heads / c->num_kv_heads;
   l.passes = (l.group + kCaHeads - 1) / kCaHeads;
   l.pitch = l.group <= 8 ? 8 : kCaHeads;
-  const long long blocks = (long long)c->batch * c->num_kv_heads * l.passes * (c->capacity / kBlockRows);
+  const long long blocks = (long long)c->batch * c->num_kv_heads * l.passes * (c->capacity / kBlockRows + kCaStart);
   l.grid = blocks < kCaGrid ? (int)blocks : kCaGrid;
   const size_t slots = (size_t)l.grid + (size_t)c->batch * c->num_kv_heads * l.passes;
   size_t at = 0;
@@ -928,7 +928,7 @@ st3_status check_heads(const st3_cache* c, int heads) {
   if (heads < 1 || heads % c->num_kv_heads) return ST3_ERR_INVALID_ARG;
   if (heads / c->num_kv_heads > 1024 || (long long)c->batch * heads * c->capacity > 0x7fffffffffLL) return ST3_ERR_UNSUPPORTED;
   const long long passes = (heads / c->num_kv_heads + kCaHeads - 1) / kCaHeads;
-  if ((long long)c->batch * c->num_kv_heads * passes * (c->capacity / kBlockRows) > 0x3fffffffLL) return ST3_ERR_UNSUPPORTED;
+  if ((long long)c->batch * c->num_kv_heads * passes * (c->capacity / kBlockRows + kCaStart) > 0x3fffffffLL) return ST3_ERR_UNSUPPORTED;
   if (heads / c->num_kv_heads + c->capacity / ca_chunk(4) + 1 > 65535) return ST3_ERR_UNSUPPORTED;
   return ST3_OK;
 }

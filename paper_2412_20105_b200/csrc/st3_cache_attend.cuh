@@ -25,6 +25,7 @@ constexpr int kCaGrid = 2 * 148;       // one wave
 constexpr int kCaConsumers = 4;
 constexpr int kCaThreads = (kCaConsumers + 1) * 32;
 constexpr int kCaHeads = 16;           // query heads of one pass over a group's rows; larger groups take several
+constexpr int kCaStart = 1;            // units of a pair beside its blocks
 constexpr int kCaMergeThreads = 128;
 // Rows of the second launch's blocks that add weights: one round of loads, or two where blocks are many.
 __host__ __device__ constexpr int ca_chunk(int split) { return split == 4 ? 512 : 1024; }
@@ -65,6 +66,9 @@ __device__ __forceinline__ int run_of(int total, int x, int grid) { return (int)
 __device__ __forceinline__ int blocks_of(const CacheAttendParams& p, int b) {
   return (clamp_rows(p.held[b], p.c.cap) + kBlockRows - 1) / kBlockRows;
 }
+// Runs are counted in units: a pair's blocks, and kCaStart in front of them for what a segment costs beside its blocks (queries and
+// scales to fetch, sums to join), so that runs of many short pairs are not the last ones to end.
+__device__ __forceinline__ int units_of(int blocks) { return blocks ? blocks + kCaStart : 0; }
 
 __device__ __forceinline__ void tma_rows(void* dst, const CUtensorMap* map, int row, uint64_t* bar) {
   asm volatile(
@@ -163,7 +167,7 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
     if (b < p.c.batch) {
-      mine += blocks_of(p, b);
+      mine += units_of(blocks_of(p, b));
       if (blockIdx.x == 0 && p.status && p.held[b] != clamp_rows(p.held[b], p.c.cap)) atomicOr(p.status, ST3_DEV_RANGE);
     }
   }
@@ -182,16 +186,16 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     total += s_int[w];
   }
   total *= pairs;
-  before *= pairs;   // blocks of all pairs in front of this thread's first sequence
+  before *= pairs;   // units of all pairs in front of this thread's first sequence
   const int grid = min(p.grid, total);
   const bool works = (int)blockIdx.x < grid;
   const int x0 = works ? run_start(total, blockIdx.x, grid) : 0, x1 = works ? run_start(total, blockIdx.x + 1, grid) : 0;
   if (x0 < x1 && x0 >= before && x0 < before + mine * pairs) {
     int b = tid * per;
     for (;; ++b) {
-      const int nb = blocks_of(p, b) * pairs;
-      if (x0 < before + nb) break;
-      before += nb;
+      const int n = units_of(blocks_of(p, b)) * pairs;
+      if (x0 < before + n) break;
+      before += n;
     }
     s_int[6] = b;
     s_int[7] = before;
@@ -207,10 +211,11 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       bool ok = true;
       int stage = 0, parity = 1, issued = 0;
       while (x < x1 && ok) {
-        int nb = blocks_of(p, b);
-        while (x >= seq0 + nb * pairs) { seq0 += nb * pairs; nb = blocks_of(p, ++b); }
-        const int pair = (x - seq0) / nb, head = pair / p.passes;
-        const int i0 = x - seq0 - pair * nb, i1 = min(nb, i0 + x1 - x);
+        int units = units_of(blocks_of(p, b));
+        while (x >= seq0 + units * pairs) { seq0 += units * pairs; units = units_of(blocks_of(p, ++b)); }
+        const int pair = (x - seq0) / units, head = pair / p.passes;
+        const int u = x - seq0 - pair * units, take = min(units - u, x1 - x);
+        const int i0 = max(u - kCaStart, 0), i1 = u + take - kCaStart;   // none, where the run holds a pair's start only
         const int row = (b * p.c.heads + head) * p.c.cap;
         for (int i = i0; i < i1; ++i) {
           if (!ca_wait(&empty[stage], parity) || *fail) { ok = false; break; }
@@ -221,7 +226,7 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           ++issued;
           if (++stage == L::kStages) { stage = 0; parity ^= 1; }
         }
-        x += i1 - i0;
+        x += take;
       }
       if (!ok) {
         *fail = 1;
@@ -249,16 +254,25 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   using Four = typename std::conditional<sizeof(T) == 2, uint2, float4>::type;
   Four raw[kTiles][kSteps];   // queries: head g, dims 16 i + 4 t .. + 3
   float ks32, vs32;           // the scales of 32 blocks, one a lane
-  auto request = [&] {
-    int nb = blocks_of(p, b);
-    while (x >= seq0 + nb * pairs) { seq0 += nb * pairs; nb = blocks_of(p, ++b); }
-    const int pair = (x - seq0) / nb, head = pair / p.passes;
+  auto request = [&] {   // the run's next segment; false at its end
+    int units = 0, pair = 0, i0 = 0, i1 = 0;
+    do {
+      if (x >= x1) return false;
+      units = units_of(blocks_of(p, b));
+      while (x >= seq0 + units * pairs) { seq0 += units * pairs; units = units_of(blocks_of(p, ++b)); }
+      pair = (x - seq0) / units;
+      const int u = x - seq0 - pair * units, take = min(units - u, x1 - x);
+      i0 = max(u - kCaStart, 0);
+      i1 = u + take - kCaStart;
+      x += take;
+    } while (i1 <= i0);
+    const int head = pair / p.passes;
     seg.b = b;
     seg.pair = pair;
     seg.h0 = (pair - head * p.passes) * kCaHeads;
     seg.heads = min(p.group - seg.h0, kCaHeads);   // of this pass
-    seg.i0 = x - seq0 - pair * nb;
-    seg.i1 = min(nb, seg.i0 + x1 - x);
+    seg.i0 = i0;
+    seg.i1 = i1;
     seg.held = clamp_rows(p.held[b], p.c.cap);
     seg.bh = (size_t)b * p.c.heads + head;
     const size_t at = seg.bh * (p.c.cap / kBlockRows) + min(seg.i0 + lane, seg.i1 - 1);
@@ -274,8 +288,9 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         if (live) raw[n][i] = *reinterpret_cast<const Four*>(src + 16 * i);
       }
     }
+    return true;
   };
-  request();
+  if (!request()) return;
   while (true) {
     const Segment now = seg;
     const int i0 = now.i0, i1 = now.i1, heads = now.heads, h0 = now.h0, held = now.held;
@@ -455,11 +470,9 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       *fail = 1;
       if (lane == 0 && p.status) atomicOr(p.status, ST3_DEV_COPY_TIMEOUT);
     }
-    x += i1 - i0;
-    const bool more = x < x1;
     // ahead of the sums where the registers allow it: a round trip under them
     constexpr bool kEarly = sizeof(T) == 2 && kTiles == 1;
-    if (kEarly && ok && more) request();
+    bool more = kEarly && ok && request();
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
@@ -518,8 +531,8 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         }
       }
     }
+    if (!kEarly) more = request();
     if (!more) break;
-    if (!kEarly) request();
   }
 }
 
@@ -541,7 +554,7 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
   const int b = bh / p.c.heads, head = bh - b * p.c.heads, pairs = p.c.heads * p.passes;
   int all = 0, below = 0;
   for (int i = tid; i < p.c.batch; i += kCaMergeThreads) {
-    const int n = blocks_of(p, i);
+    const int n = units_of(blocks_of(p, i));
     all += n;
     if (i < b) below += n;
   }
@@ -571,7 +584,7 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
         for (int e = lane; e < D; e += 32) store_out(dst + e, 0.f);
       return;
     }
-    const int x = below * pairs + pair * nb;
+    const int x = below * pairs + pair * units_of(nb) + kCaStart;   // the pair's first block
     const int c0 = run_of(total, x, grid), n = live ? run_of(total, x + nb - 1, grid) - c0 + 1 : 0;   // n <= grid segments
     const size_t slot0 = ((size_t)b * pairs + pair + c0) * p.pitch + h - pass * kCaHeads;
     const float* ml = p.part_ml + slot0 * 3;
@@ -662,7 +675,7 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
     __syncthreads();
     for (int h = h0 + warp; h < min(p.group, h0 + 128); h += kWarps4) {
       const int pass = h / kCaHeads, pair = head * p.passes + pass;
-      const int x = below * pairs + pair * nb;
+      const int x = below * pairs + pair * units_of(nb) + kCaStart;
       const int c0 = run_of(total, x, grid), n = run_of(total, x + nb - 1, grid) - c0 + 1;
       const float* ml = p.part_ml + (((size_t)b * pairs + pair + c0) * p.pitch + h - pass * kCaHeads) * 3;
       float a = -INFINITY, sum = 0.f;
