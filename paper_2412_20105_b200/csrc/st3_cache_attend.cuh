@@ -63,9 +63,9 @@ struct CaLayout {
 __device__ __forceinline__ int run_start(int total, int c, int grid) { return (int)((long long)total * c / grid); }
 // The thread block whose run holds block x.
 __device__ __forceinline__ int run_of(int total, int x, int grid) { return (int)((((long long)x + 1) * grid - 1) / total); }
-__device__ __forceinline__ int blocks_of(const CacheAttendParams& p, int b) {
-  return (clamp_rows(p.held[b], p.c.cap) + kBlockRows - 1) / kBlockRows;
-}
+// Rows held, from L2: the joining launch reads them ahead of its wait, when nothing says that this SM's L1 is not older than them.
+__device__ __forceinline__ int held_of(const CacheAttendParams& p, int b) { return clamp_rows(__ldcg(p.held + b), p.c.cap); }
+__device__ __forceinline__ int blocks_of(const CacheAttendParams& p, int b) { return (held_of(p, b) + kBlockRows - 1) / kBlockRows; }
 // Runs are counted in units: a pair's blocks, and kCaStart in front of them for what a segment costs beside its blocks (queries and
 // scales to fetch, sums to join), so that runs of many short pairs are not the last ones to end.
 __device__ __forceinline__ int units_of(int blocks) { return blocks ? blocks + kCaStart : 0; }
@@ -273,7 +273,7 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     seg.heads = min(p.group - seg.h0, kCaHeads);   // of this pass
     seg.i0 = i0;
     seg.i1 = i1;
-    seg.held = clamp_rows(p.held[b], p.c.cap);
+    seg.held = held_of(p, b);
     seg.bh = (size_t)b * p.c.heads + head;
     const size_t at = seg.bh * (p.c.cap / kBlockRows) + min(seg.i0 + lane, seg.i1 - 1);
     ks32 = p.c.scale[0][at];
@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
     all += n;
     if (i < b) below += n;
   }
-  const int held = clamp_rows(p.held[b], p.c.cap), nb = (held + kBlockRows - 1) / kBlockRows;
+  const int held = held_of(p, b), nb = (held + kBlockRows - 1) / kBlockRows;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     all += __shfl_xor_sync(0xffffffffu, all, o);
