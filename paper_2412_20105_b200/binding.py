@@ -396,8 +396,9 @@ class Cache:
 
     `Cache(k, v, k_scale, v_scale, ids, weights)` wraps existing tensors, `Cache.empty(...)` allocates them.  `status` is
     the device status word that the calls report into.  How many rows each sequence holds is the caller's to keep: an
-    int32 tensor [batch] that goes into the calls.  The workspaces are kept between calls: use a Cache on one stream
-    at a time."""
+    int32 tensor [batch] that goes into the calls.  The workspaces are kept between calls (one for each number of query
+    heads, with and without weights, and one for evictions): use a Cache on one stream at a time, and order replays of
+    graphs that hold its calls against them and each other."""
 
     def __init__(self, k, v, k_scale, v_scale, ids, weights):
         import torch
@@ -415,8 +416,7 @@ class Cache:
                               _dense(weights, codes[:3], f32, index, "weights"))
         self.batch, self.num_kv_heads, self.capacity, self.head_dim = n, heads, cap, dim
         self.status = torch.zeros(1, dtype=i32, device=k.device)
-        self._attend_ws = self._evict_ws = None
-        self._attend_bytes = {}
+        self._workspaces = {}     # what for -> (tensor, address, bytes); never let go, as a captured graph may hold its address
 
     @classmethod
     def empty(cls, batch, num_kv_heads, head_dim, capacity, device="cuda:0"):
@@ -432,10 +432,12 @@ class Cache:
     def _count(self, t, what):
         return None if t is None else _dense(t, (self.batch,), self.torch.int32, self._index, what)
 
-    def _workspace(self, ws, nbytes):
-        if ws is None or ws.numel() < nbytes + 256:
+    def _workspace(self, key, size):
+        if key not in self._workspaces:
+            nbytes = size()
             ws = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
-        return ws, (ws.data_ptr() + 255) // 256 * 256
+            self._workspaces[key] = ws, (ws.data_ptr() + 255) // 256 * 256, nbytes
+        return self._workspaces[key][1:]
 
     def store(self, k, v, cu, start=None, pos=None):
         """Rows cu[s] .. cu[s+1]-1 of k and v ([tokens, kv heads, dim]) go behind the start[s] rows of sequence s."""
@@ -458,23 +460,18 @@ class Cache:
             wi = _dense(self.weights if weights_in is None else weights_in, self.weights.shape, self.torch.float32, self._index, "weights_in")
             wo = _dense(weights_out, self.weights.shape, self.torch.float32, self._index, "weights_out")
         key = (heads, wo is not None)
-        if key not in self._attend_bytes:
-            self._attend_bytes[key] = st3_cache_attend_workspace(self.desc, *key)
-        self._attend_ws, ws = self._workspace(self._attend_ws, self._attend_bytes[key])
+        ws, nbytes = self._workspace(key, lambda: st3_cache_attend_workspace(self.desc, *key))
         st3_cache_attend(self.desc, _dense(q, shape, q.dtype, self._index, "q"), _dense(out, shape, q.dtype, self._index, "out"),
-                         dt, heads, self._count(held, "held"), wi, wo, ws, self._attend_bytes[key], self.status.data_ptr(),
-                         _stream_of(self._index))
+                         dt, heads, self._count(held, "held"), wi, wo, ws, nbytes, self.status.data_ptr(), _stream_of(self._index))
 
     def evict(self, held, seen, keep, recent=0, into=None, held_out=None):
         """Cuts every head to `keep` rows, in place or into another Cache; returns the new numbers of rows held."""
         to = self if into is None else into
         if held_out is None:
             held_out = self.torch.empty_like(held)
-        if self._evict_ws is None:
-            self._evict_bytes = st3_cache_evict_workspace(self.desc)
-        self._evict_ws, ws = self._workspace(self._evict_ws, self._evict_bytes)
+        ws, nbytes = self._workspace("evict", lambda: st3_cache_evict_workspace(self.desc))
         st3_cache_evict(self.desc, to.desc, self._count(held, "held"), self._count(seen, "seen"), keep, recent,
-                        self._count(held_out, "held_out"), ws, self._evict_bytes, self.status.data_ptr(), _stream_of(self._index))
+                        self._count(held_out, "held_out"), ws, nbytes, self.status.data_ptr(), _stream_of(self._index))
         return held_out
 
     def rows(self, held, num_rows, first=None, dtype=None):

@@ -399,6 +399,20 @@ def test_ties_and_weights_that_are_not_ordinary(case):
 
 
 @gpu
+@pytest.mark.parametrize("n,keep", [(2000, 700), (9500, 4000)])
+@pytest.mark.parametrize("values", [1, 2, 40])
+def test_more_ties_than_are_ranked_one_against_the_other(n, keep, values):
+    """Thousands of rows share the weight of the cut: the earlier positions stay.  Staged in shared memory and beyond that."""
+    p = Pair(1, 2, 64, n, seed=values)
+    p.store([n])
+    p.set_weights(lambda b, h, m: p.g.integers(0, values, size=m) * 0.5)
+    p.evict(keep + n // 4, 0)               # positions no longer ascend
+    p.set_weights(lambda b, h, m: p.g.integers(0, values, size=m) * -0.25)
+    p.evict(keep, 50)
+    p.check()
+
+
+@gpu
 def test_long_heads_and_nothing_to_evict():
     p = Pair(2, 1, 64, 9000, seed=1)
     p.store([9000, 50])
@@ -473,6 +487,52 @@ def test_captured_steps_replay_and_other_streams():
         results.append(outs + [p.cache.weights[:, :, :100].clone(), p.cache.ids[:, :, :100].clone(), held.clone()])
         assert int(p.cache.status) == 0
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@gpu
+def test_a_graph_keeps_its_workspace_when_other_calls_need_more():
+    p = Pair(2, 2, 64, 400, seed=4)
+    p.store([380, 111])
+    g = torch.Generator().manual_seed(2)
+    q, out = torch.randn(2, 4, 64, generator=g).bfloat16().cuda(), torch.empty(2, 4, 64, dtype=torch.bfloat16, device="cuda")
+    held, w = _i32([380, 111]), torch.zeros_like(p.cache.weights)
+    zeros = torch.zeros_like(w)
+    p.cache.attend(q, held, out, weights_out=w, weights_in=zeros)
+    want, want_w = out.clone(), w.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.cache.attend(q, held, out, weights_out=w, weights_in=zeros)
+    many = torch.randn(2, 64, 64, generator=g).bfloat16().cuda()
+    p.cache.attend(many, held, torch.empty_like(many), weights_out=torch.empty_like(w), weights_in=zeros)
+    junk = [torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda") for _ in range(64)]     # whatever was let go is taken
+    out.zero_()
+    graph.replay()
+    assert torch.equal(out, want) and torch.equal(w, want_w) and len(junk) == 64
+
+
+@gpu
+def test_two_caches_on_two_streams():
+    ps = [Pair(2, 4, 128, 2000, seed=s) for s in (1, 2)]
+    g = torch.Generator().manual_seed(7)
+    q = torch.randn(2, 16, 128, generator=g).bfloat16().cuda()
+    want = []
+    for p in ps:
+        p.store([1999, 1500])
+        out = torch.empty_like(q)
+        p.cache.attend(q, _i32([1999, 1500]), out)
+        want.append(out)
+    held = _i32([1999, 1500])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ps]
+    got = [[] for _ in ps]
+    for _ in range(10):
+        for p, st, outs in zip(ps, streams, got):
+            with torch.cuda.stream(st):
+                out = torch.empty_like(q)
+                p.cache.attend(q, held, out)
+                outs.append(out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for outs, w in zip(got, want) for o in outs)
 
 
 @gpu
