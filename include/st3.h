@@ -299,7 +299,7 @@ st3_status st3_attend_noalloc(const void* q, const void* k, const void* v, void*
  * head h reads key/value head h / (num_heads / num_kv_heads).  Neither call needs a context or a workspace. */
 typedef struct {
   int32_t num_seqs;      /* sequences (0 allowed)                                                   */
-  int32_t total;         /* tokens of all sequences = cu[num_seqs] (0 allowed)                      */
+  int32_t total;         /* rows of the packed tensors, at least cu[num_seqs] (0 allowed)           */
   int32_t num_heads;     /* query heads, a multiple of num_kv_heads                                 */
   int32_t num_kv_heads;
   int32_t head_dim;      /* 64 or 128                                                               */
@@ -312,7 +312,8 @@ typedef struct {
 
 /* Causal attention inside each sequence (Eq. 2: A = Softmax((Q K^T + M)/sqrt(D)), out = A V) on the tcgen05 tensor
  * cores.
- *   cu          dev int32 [num_seqs + 1], ascending from 0 to total
+ *   cu          dev int32 [num_seqs + 1], ascending, 0 <= cu[0], cu[num_seqs] <= total.  Rows of out and lse that belong to
+ *               no sequence are left as they were.
  *   out         dev, like q with its own strides
  *   lse         dev fp32 [num_heads][total], may be NULL: log sum_j exp(q_i . k_j / sqrt(D)) of every row
  *   dev_status  dev int, may be NULL: ST3_DEV_COPY_TIMEOUT as in st3_prefill_attend, ST3_DEV_RANGE if cu is not what it

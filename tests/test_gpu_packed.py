@@ -62,7 +62,7 @@ def _check_attend(q, k, v, lens, out, lse):
 
 SHAPES = [([1], 2, 1, 128), ([1, 37, 130], 8, 2, 64), ([128], 4, 4, 128), ([129, 127, 128], 4, 2, 128), ([0, 5, 0, 0, 64, 0], 6, 1, 64),
           ([257, 256, 255], 3, 1, 128), ([300, 1, 511, 513], 5, 5, 64), ([675, 640], 8, 2, 128), ([1100], 14, 2, 128),
-          ([3] * 90 + [200], 4, 1, 64)]
+          ([3] * 90 + [200], 4, 1, 64), ([200, 65], 1, 1, 64), ([130], 16, 1, 128)]
 
 
 @gpu
@@ -155,6 +155,43 @@ def test_outputs_with_strides_and_without_sums():
         assert torch.equal(out, want)
         out.fill_(7.0)
         assert bool((room == 7.0).all())         # nothing beside the view was written
+
+
+@gpu
+def test_rows_of_no_sequence_are_left_as_they_were():
+    """A padded batch: tokens ahead of the first sequence and behind the last one, with anything in them."""
+    lens, before, after = [100, 0, 61], 5, 200
+    for heads, kv in ((4, 2), (3, 3)):
+        q, k, v = _inputs(lens, heads, kv, 64, layout="dense")
+        want, lse = _attend(q, k, v, lens)
+        pad = lambda x: torch.cat([torch.full_like(x[:before], float("nan")), x, torch.full((after,) + x.shape[1:], float("inf"), dtype=x.dtype, device="cuda")])
+        out = torch.full((before + 161 + after, heads, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        sums = torch.full((heads, out.shape[0]), 7.0, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        B.packed_attend(pad(q), pad(k), pad(v), _starts(lens) + before, out, sums, status)
+        assert int(status) == 0
+        mine = slice(before, before + 161)
+        assert torch.equal(out[mine], want) and torch.equal(sums[:, mine], lse)
+        assert bool((out[:before] == 7).all()) and bool((out[before + 161:] == 7).all()) and bool((sums[:, before + 161:] == 7).all())
+        w, w2 = torch.full((3, kv, 128), -1.0, device="cuda"), torch.full((3, kv, 128), -1.0, device="cuda")
+        B.packed_weights(q, k, lse, _starts(lens), w)
+        B.packed_weights(pad(q), pad(k), sums, _starts(lens) + before, w2, 0, status)
+        assert torch.equal(w, w2) and int(status) == 0
+
+
+@gpu
+def test_thousands_of_sequences_most_of_them_empty():
+    g = np.random.default_rng(5)
+    lens = [int(x) for x in g.integers(0, 3, size=3001) * (g.random(3001) < 0.3)]
+    q, k, v = _inputs(lens, 4, 2, 64, seed=8)
+    out, lse = _attend(q, k, v, lens)
+    _check_attend(q, k, v, lens, out, lse)
+    w = torch.full((3001, 2, 64), -1.0, device="cuda")
+    B.packed_weights(q, k, lse, _starts(lens), w)
+    want = O.packed_weights(_f64(q), _f64(k), _f64(lse), lens)
+    got = w.cpu().numpy()
+    for s, n in enumerate(lens):
+        assert np.allclose(got[s, :, :n], want[s], rtol=1e-4) and np.all(got[s, :, n:] == -1)
 
 
 @gpu
