@@ -10,20 +10,27 @@
 
 namespace {
 
-// A launch that may be set up while the one ahead of it in the stream still runs; the kernel waits for it itself.
+// A launch that may be set up while the one ahead of it in the stream still runs; the kernel waits for it itself.  Its blocks
+// come in clusters of `cluster`, if that is more than one.
 template <typename... P, typename... A>
-st3_status launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const A&... args) {
-  cudaLaunchAttribute attr[1];
+st3_status launch_clusters(int cluster, void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const A&... args) {
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? ST3_OK : ST3_ERR_CUDA;
+}
+template <typename... P, typename... A>
+st3_status launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const A&... args) {
+  return launch_clusters(1, kernel, grid, block, smem, stream, args...);
 }
 
 // Raises a kernel's limit of dynamic shared memory, once on each device (a call costs as much as a fifth of a launch).  Two

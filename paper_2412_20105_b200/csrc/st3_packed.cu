@@ -6,7 +6,8 @@
 // of heads, 256 queries of one head) against key/value tiles of 128 rows; for the weights 256 keys of a key/value
 // head against tiles of 128 queries.  A block per SM is persistent: the first item is its block index, the others are block
 // indices that it takes from the hardware's queue (cluster launch control), so that items of very different lengths
-// spread without a counter in memory and the next item's loads run under the end of this one.
+// spread without a counter in memory and the next item's loads run under the end of this one.  Where the weights have few items,
+// a cluster of blocks shares each of them instead.
 //
 // Items need no table either: sequence s has the numbers cu[s]/R + s and on (R rows an item), which are at least as many as
 // the ceil(n/R) that it needs; numbers without an item are passed over.  The weights' items go in two rounds, the longer half of
@@ -262,10 +263,11 @@ __device__ __forceinline__ bool pk_any_failed(int tile, bool failed) {
 
 // The loader's loop over items, the same for both kernels: `decode(index, item)` fills an item (false: nothing to do) and
 // `load(item)` brings its tiles.
-template <typename Decode, typename Load>
-__device__ __forceinline__ void pk_loader(PkShared& sh, int* status, Decode&& decode, Load&& load) {
+// With kOne the block has item `index` and no other.
+template <bool kOne, typename Decode, typename Load>
+__device__ __forceinline__ void pk_loader(PkShared& sh, int* status, int index, Decode&& decode, Load&& load) {
   const int lane = threadIdx.x & 31;
-  int index = blockIdx.x, slot = 0;
+  int slot = 0;
   uint32_t phase = 1, answer = 0;
   bool ok = true;
   while (true) {
@@ -280,6 +282,7 @@ __device__ __forceinline__ void pk_loader(PkShared& sh, int* status, Decode&& de
       }
       if (!ok) break;
     }
+    if (kOne) break;
     // The next item is taken when this one's last tiles have been requested, which is a few steps ahead of their use: taken any
     // earlier, it would stay with this block while others run out of work (weights of 16 x 690 tokens: 98 -> 85 us).
     if (lane == 0) {
@@ -379,8 +382,8 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     // ===================== loader =====================
     Ring<L::kStages> ring;
     int issued = 0, owned = 0;
-    pk_loader(
-        sh, p.status,
+    pk_loader<false>(
+        sh, p.status, blockIdx.x,
         [&](int index, PkItem& it) {
           const int number = index / p.pairs, pair = index - number * p.pairs;
           const int slot = p.items / p.pairs - 1 - number;    // a sequence's last rows, the longest items, first
@@ -670,7 +673,32 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[64], int part, c
   }
 }
 
-template <int D>
+// The (query tile, head) pairs that a block of a cluster takes part in, from query tile t0 on: every `ranks`-th one, ranks a power
+// of two.
+struct WeightSteps {
+  int t, g;
+  const int group, ranks;
+  __device__ __forceinline__ WeightSteps(int t0, int group_, int rank, int ranks_) : t(t0), g((rank - t0 * group_) & (ranks_ - 1)), group(group_), ranks(ranks_) { carry(); }
+  __device__ __forceinline__ void carry() { while (g >= group) { g -= group; ++t; } }
+  __device__ __forceinline__ void next() { g += ranks; carry(); }
+};
+
+__device__ __forceinline__ int cluster_rank() { int r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ int cluster_ranks() { int r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float peer_value(const float* mine, int rank) {
+  float x;
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+  return x;
+}
+
+// kSplit: an item belongs to the blocks of a cluster, which share out its steps and have no other item.  The sums are
+// joined, in the order of the blocks, through the first one's reads of the others' shared memory.
+template <int D, bool kSplit>
 __global__ void __launch_bounds__(WeightRoles::kThreads, 1)
 st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const PackedParams p) {
   using L = PkLayout<D, 2>;
@@ -682,6 +710,8 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
   const int lane = threadIdx.x & 31, warp = WeightRoles::warp();
   volatile int* fail = &sh.fail;
   const int rows = 2 * kPkRows;
+  const int ranks = kSplit ? cluster_ranks() : 1, rank = kSplit ? cluster_rank() : 0;
+  float* s_rows = reinterpret_cast<float*>(smem + L::kLse);
 
   // Query tiles start at the first query that counts.  steps[x] is the first of them that key tile x takes part in, and
   // `begin` the number of them in all.
@@ -691,8 +721,8 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
   } else if (warp == WeightRoles::kLoader) {
     Ring<L::kStages> ring;
     int issued = 0, owned = 0;
-    pk_loader(
-        sh, p.status,
+    pk_loader<kSplit>(
+        sh, p.status, blockIdx.x / ranks,
         [&](int index, PkItem& it) {
           const int number = index / p.kv_heads, head = index - number * p.kv_heads, half = p.items / p.kv_heads / 2;
           const bool second = number >= half;
@@ -705,14 +735,14 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
           }
           const int n = (it.len + rows - 1) / rows, longer = (n + 1) / 2, place = slot - (p.cu[b] / (2 * rows) + b);
           if (place < 0 || place >= (second ? n - longer : longer)) return false;
-          const int rank = second ? longer + place : place;
+          const int tile = second ? longer + place : place;
           it.seq = b;
           it.begin = p.window > 0 ? max(0, it.len - p.window) : 0;
           const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             it.head[x] = head;
-            it.first[x] = rank * rows + x * kPkRows;
+            it.first[x] = tile * rows + x * kPkRows;
             it.steps[x] = it.first[x] < it.len ? max(0, it.first[x] - it.begin) / kPkRows : tiles;
           }
           return true;
@@ -728,18 +758,17 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
           }
           ++owned;
           const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
-          for (int t = it.steps[0]; t < tiles && ok; ++t)
-            for (int g = 0; g < p.group && ok; ++g) {
-              ok = pk_wait_warp(&sh.empty[ring.stage], ring.phase ^ 1, fail);
-              if (!ok) break;
-              if (lane == 0) {
-                mbar_expect_tx(&sh.full[ring.stage], L::kTile);
-                load_tile<L::kBoxes>(smem + L::kRing + ring.stage * L::kTile, &map_q, it.head[0] * p.group + g, it.row + it.begin + t * kPkRows, &sh.full[ring.stage]);
-              }
-              __syncwarp();
-              ++issued;
-              ring.step();
+          for (WeightSteps s(it.steps[0], p.group, rank, ranks); s.t < tiles; s.next()) {
+            ok = pk_wait_warp(&sh.empty[ring.stage], ring.phase ^ 1, fail);
+            if (!ok) break;
+            if (lane == 0) {
+              mbar_expect_tx(&sh.full[ring.stage], L::kTile);
+              load_tile<L::kBoxes>(smem + L::kRing + ring.stage * L::kTile, &map_q, it.head[0] * p.group + s.g, it.row + it.begin + s.t * kPkRows, &sh.full[ring.stage]);
             }
+            __syncwarp();
+            ++issued;
+            ring.step();
+          }
           return ok;
         });
     if (lane == 0) pk_settle<L::kStages, 2>(sh, issued, owned);
@@ -757,34 +786,33 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
       const uint32_t own_buf = owned & 1, mine_lo = uniform(own_lo + own_buf * (2 * L::kTile >> 4));
       ok = pk_wait_warp(&sh.own[own_buf], (owned >> 1) & 1, fail);
       ++owned;
-      for (int t = uniform(it.steps[0]); t < tiles && ok; ++t)
-        for (int g = 0; g < p.group && ok; ++g) {
-          ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
+      for (WeightSteps s(uniform(it.steps[0]), p.group, rank, ranks); s.t < tiles && ok; s.next()) {
+        ok = pk_wait_warp(&sh.full[ring.stage], ring.phase, fail);
+        if (!ok) break;
+        const bool works = s.t >= mine;
+        const uint32_t bar = 2 * x + (use & 1);
+        if (works) {
+          ok = pk_wait_warp(&sh.taken[bar], ((use >> 1) & 1) ^ 1, fail);
           if (!ok) break;
-          const bool works = t >= mine;
-          const uint32_t bar = 2 * x + (use & 1);
-          if (works) {
-            ok = pk_wait_warp(&sh.taken[bar], ((use >> 1) & 1) ^ 1, fail);
-            if (!ok) break;
-            ++use;
-          }
-          tc_fence_after();
-          const uint32_t q_lo = uniform(ring_lo + (uint32_t)ring.stage * (L::kTile >> 4)), tS = uniform(tmem + bar * 128);
-          if (elected()) {
-            if (works) {
-#pragma unroll
-              for (int ks = 0; ks < D / 16; ++ks) {
-                const uint32_t off = ((ks >> 2) * kBox + (ks & 3) * 32) >> 4;
-                umma_bf16(tS, mine_lo + off, q_lo + off, kIdescScores, ks > 0);
-              }
-              umma_commit(&sh.scores[bar]);
-            }
-            umma_commit(&sh.empty[ring.stage]);
-            if (t == tiles - 1 && g == p.group - 1) umma_commit(&sh.own_free[own_buf]);
-          }
-          __syncwarp();
-          ring.step();
+          ++use;
         }
+        tc_fence_after();
+        const uint32_t q_lo = uniform(ring_lo + (uint32_t)ring.stage * (L::kTile >> 4)), tS = uniform(tmem + bar * 128);
+        if (elected()) {
+          if (works) {
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint32_t off = ((ks >> 2) * kBox + (ks & 3) * 32) >> 4;
+              umma_bf16(tS, mine_lo + off, q_lo + off, kIdescScores, ks > 0);
+            }
+            umma_commit(&sh.scores[bar]);
+          }
+          umma_commit(&sh.empty[ring.stage]);
+          if (!kSplit && s.t == tiles - 1 && s.g == p.group - 1) umma_commit(&sh.own_free[own_buf]);
+        }
+        __syncwarp();
+        ring.step();
+      }
     }
     if (!ok || *fail) pk_give_up(sh, p.status);
   } else {
@@ -792,7 +820,6 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     const int group = warp >> 2, x = group >> 1, half = group & 1, w32 = (warp & 3) * 32, r = w32 + lane;
     const uint32_t lane_addr = (uint32_t)w32 << 16;
     const float sc = kLog2e * rsqrtf((float)D);
-    float* s_rows = reinterpret_cast<float*>(smem + L::kLse);
     float* s_lse = s_rows + group * 128;   // two buffers of this warpgroup's 64 queries
     int slot = 0;
     uint32_t phase = 0, use = 0;
@@ -814,36 +841,37 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         const int q = begin + t * kPkRows + half * 64 + r;
         return r < 64 && t < tiles && q < len ? lse[(size_t)g * p.total + q] : 0.f;
       };
-      float next = load_lse(t0, 0);
-      for (int t = t0; t < tiles && ok; ++t) {
-        const int q0 = begin + t * kPkRows + half * 64, valid = len - q0;
-        for (int g = 0; g < p.group; ++g) {
-          const uint32_t buf = use & 1;
-          if (r < 64) s_lse[buf * 64 + r] = -kLog2e * next;
-          if (pk_any_failed(x, !ok)) { ok = false; left = true; break; }
-          next = g + 1 < p.group ? load_lse(t, g + 1) : load_lse(t + 1, 0);
-          ok = pk_wait_warp(&sh.scores[2 * x + buf], (use >> 1) & 1, fail);
-          if (!ok) { *fail = 1; continue; }   // told to the others at the next barrier
-          ++use;
-          tc_fence_after();
-          uint32_t v[64];
-          tmem_ld64(tmem + (2 * x + buf) * 128 + half * 64 + lane_addr, v);
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + buf]);   // the next product may overwrite it
+      WeightSteps s(t0, p.group, rank, ranks);
+      float next = load_lse(s.t, s.g);
+      while (s.t < tiles && ok) {
+        const int t = s.t, q0 = begin + t * kPkRows + half * 64, valid = len - q0;
+        const uint32_t buf = use & 1;
+        if (r < 64) s_lse[buf * 64 + r] = -kLog2e * next;
+        if (pk_any_failed(x, !ok)) { ok = false; left = true; break; }
+        s.next();
+        next = load_lse(s.t, s.g);
+        ok = pk_wait_warp(&sh.scores[2 * x + buf], (use >> 1) & 1, fail);
+        if (!ok) { *fail = 1; break; }   // told to the others at the next barrier
+        ++use;
+        tc_fence_after();
+        uint32_t v[64];
+        tmem_ld64(tmem + (2 * x + buf) * 128 + half * 64 + lane_addr, v);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + buf]);   // the next product may overwrite it
 #pragma unroll
-          for (int part = 0; part < 2; ++part) {   // 32 queries, of which none, all or some count for this warp's keys
-            const int c0 = part * 32, lo = key - q0 - c0, hi = valid - c0;
-            const int warp_lo = first + w32 - q0 - c0;   // the warp's first key; its last is 31 further
-            if (warp_lo > 31 || hi <= 0) continue;
-            if (warp_lo + 31 <= 0 && hi >= 32) add_weights<false>(v, part, s_lse + buf * 64 + c0, sc, 0, 32, acc);
-            else add_weights<true>(v, part, s_lse + buf * 64 + c0, sc, lo, hi, acc);
-          }
+        for (int part = 0; part < 2; ++part) {   // 32 queries, of which none, all or some count for this warp's keys
+          const int c0 = part * 32, lo = key - q0 - c0, hi = valid - c0;
+          const int warp_lo = first + w32 - q0 - c0;   // the warp's first key; its last is 31 further
+          if (warp_lo > 31 || hi <= 0) continue;
+          if (warp_lo + 31 <= 0 && hi >= 32) add_weights<false>(v, part, s_lse + buf * 64 + c0, sc, 0, 32, acc);
+          else add_weights<true>(v, part, s_lse + buf * 64 + c0, sc, lo, hi, acc);
         }
-        // 32-bit sums of at most 64 * group terms each, added up here
-        sum += (sum2(acc[0]) + sum2(acc[1])) + (sum2(acc[2]) + sum2(acc[3]));
+        if (s.t != t) {   // 32-bit sums of at most 64 * group terms each, added up here
+          sum += (sum2(acc[0]) + sum2(acc[1])) + (sum2(acc[2]) + sum2(acc[3]));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
+          for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
+        }
       }
       const int seq = it.seq, head = it.head[0];
       pk_release(sh, slot, phase);
@@ -853,10 +881,24 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
       if (left || pk_any_failed(x, !ok)) { ok = false; break; }   // all of them have read their lse
       if (half == 1) *s_sum = sum;
       asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
-      if (half == 0 && key < len) p.weights[((size_t)seq * p.kv_heads + head) * p.capacity + key] = sum + *s_sum;
+      if (kSplit && half == 0) s_rows[2 * x * 128 + r] = sum + *s_sum;   // in the place of the first half's lse
+      if (!kSplit && half == 0 && key < len) p.weights[((size_t)seq * p.kv_heads + head) * p.capacity + key] = sum + *s_sum;
       asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
     }
     if (!ok) *fail = 1;
+  }
+  if (kSplit) {
+    __syncwarp();
+    cluster_sync();
+    const PkItem& it = sh.item[0];
+    const int x = threadIdx.x >> 7, r = threadIdx.x & 127;
+    if (rank == 0 && x < 2 && !it.stop && !*fail && it.first[x] + r < it.len) {
+      float sum = 0.f;
+      for (int c = 0; c < ranks; ++c) sum += peer_value(s_rows + 2 * x * 128 + r, c);
+      p.weights[((size_t)it.seq * p.kv_heads + it.head[0]) * p.capacity + it.first[x] + r] = sum;
+    }
+    __syncwarp();
+    cluster_sync();   // the others' shared memory stays until it has been read
   }
   pk_end<WeightRoles>(sh, tmem);
 }
@@ -904,9 +946,34 @@ st3_status attend_launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUt
   return launch(st3_packed_attend_kernel<D>, dim3((unsigned)d.items), dim3(AttendRoles::kThreads), PkLayout<D, 1>::kTotal, s, mq, mk, mv, d);
 }
 template <int D>
-st3_status weights_launch(const CUtensorMap& mq, const CUtensorMap& mk, const PackedParams& d, cudaStream_t s) {
-  if (!allow_smem<st3_packed_weights_kernel<D>>(PkLayout<D, 2>::kTotal)) return ST3_ERR_CUDA;
-  return launch(st3_packed_weights_kernel<D>, dim3((unsigned)d.items), dim3(WeightRoles::kThreads), PkLayout<D, 2>::kTotal, s, mq, mk, d);
+st3_status weights_launch(const CUtensorMap& mq, const CUtensorMap& mk, const PackedParams& d, int split, cudaStream_t s) {
+  const dim3 grid((unsigned)(d.items * split)), block(WeightRoles::kThreads);
+  constexpr int smem = PkLayout<D, 2>::kTotal;
+  if (split > 1) {
+    if (!allow_smem<st3_packed_weights_kernel<D, true>>(smem)) return ST3_ERR_CUDA;
+    return launch_clusters(split, st3_packed_weights_kernel<D, true>, grid, block, smem, s, mq, mk, d);
+  }
+  if (!allow_smem<st3_packed_weights_kernel<D, false>>(smem)) return ST3_ERR_CUDA;
+  return launch(st3_packed_weights_kernel<D, false>, grid, block, smem, s, mq, mk, d);
+}
+
+// Blocks that share an item of the weights.  A prompt alone has fewer items than the GPU has SMs, and the longest, the first
+// keys' with all queries, takes as long as a block needs for them.  Shared by the blocks of a cluster, items become more and
+// shorter; against that stand a block's start (2 us, which the queue hides) and that it is done once for each of the blocks.
+// So: as many as the SMs hold, or up to about three rounds of blocks where an item has steps enough (us, shared by 1 / 2 / 4 / 8
+// blocks; 32 heads on 8, D = 128: 700 tokens 37 / 22 / 14 / 17, 2 500: 121 / 67 / 59 / 81, 4 000: 195 / 104 / 122; 8 heads on 2,
+// D = 64: 700: 36 / 20 / 13 / 9; one head to a group, 32 heads: 700: 13 / 15 / 25).  Clusters of eight fit less well: 16 of
+// them take two rounds.
+int weights_split(const PackedParams& d) {
+  const long long items = ((long long)d.total / (2 * kPkRows) + d.num_seqs) * d.kv_heads;   // at most
+  const int longest = d.total / d.num_seqs + 1, queries = d.window > 0 ? min(d.window, longest) : longest;   // for even lengths
+  const long long steps = (long long)((queries + kPkRows - 1) / kPkRows) * d.group;
+  int split = 1;
+  for (int blocks = 2; blocks <= 8 && blocks <= steps; blocks *= 2) {
+    const int most = blocks < 8 ? (steps < 16 ? 148 : 400) : (steps < 40 ? 112 : 200);
+    if (items * blocks <= most) split = blocks;
+  }
+  return split;
 }
 
 }  // namespace
@@ -953,5 +1020,6 @@ extern "C" st3_status st3_packed_weights(const st3_packed* p, const void* q, con
   d.pairs = d.kv_heads;
   d.items = 2 * (d.total / (4 * kPkRows) + d.num_seqs) * d.pairs;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  return p->head_dim == 128 ? weights_launch<128>(mq, mk, d, s) : weights_launch<64>(mq, mk, d, s);
+  const int split = weights_split(d);
+  return p->head_dim == 128 ? weights_launch<128>(mq, mk, d, split, s) : weights_launch<64>(mq, mk, d, split, s);
 }

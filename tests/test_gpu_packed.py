@@ -190,7 +190,7 @@ def test_thousands_of_sequences_most_of_them_empty():
     B.packed_weights(q, k, lse, _starts(lens), w)
     want = O.packed_weights(_f64(q), _f64(k), _f64(lse), lens)
     got = w.cpu().numpy()
-    for s, n in enumerate(lens):
+    for s, n in enumerate(lens):   # logits and sums below 24 together: 2^-18 * (1 + 24) < 1e-4
         assert np.allclose(got[s, :, :n], want[s], rtol=1e-4) and np.all(got[s, :, n:] == -1)
 
 
@@ -364,3 +364,24 @@ def test_tensors_of_the_wrong_kind_are_refused():
             f()
     with pytest.raises(B.St3Error):
         B.packed_attend(q.float(), k.float(), v.float(), cu, out.float(), lse)
+
+
+@gpu
+@pytest.mark.parametrize("lens,heads,kv,dim,window", [
+    ([700], 32, 8, 128, 0), ([700], 4, 1, 64, 0), ([1300], 6, 2, 64, 0), ([257], 3, 3, 64, 0), ([1], 16, 1, 128, 0), ([130], 16, 1, 64, 1),
+    ([2000, 3], 2, 1, 64, 900), ([500, 0, 700], 8, 4, 64, 0), ([1500], 8, 1, 128, 200)])
+def test_weights_of_few_items_are_shared_by_blocks(lens, heads, kv, dim, window):
+    """A prompt or two: the steps of an item go to 2, 4 or 8 blocks, whose sums are joined in one order."""
+    q, k, v = _inputs(lens, heads, kv, dim, seed=3)
+    lse = _attend(q, k, v, lens)[1]
+    cap = -(-max(lens) // 64) * 64
+    w = torch.full((len(lens), kv, cap), -1.0, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.packed_weights(q, k, lse, _starts(lens), w, window, status)
+    again = torch.full_like(w, -1.0)
+    B.packed_weights(q, k, lse, _starts(lens), again, window)
+    assert torch.equal(w, again) and int(status) == 0
+    want = O.packed_weights(_f64(q), _f64(k), _f64(lse), lens, window)
+    got = w.cpu().numpy()
+    for s, n in enumerate(lens):   # logits and sums below 24 together: 2^-18 * (1 + 24) < 1e-4
+        assert np.allclose(got[s, :, :n], want[s], rtol=1e-4, atol=1e-30) and np.all(got[s, :, n:] == -1)
