@@ -10,6 +10,7 @@
 // before the first access to memory, in every block.
 #include "st3_common.cuh"
 
+#include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -367,7 +368,9 @@ struct EvictParams {
   int* held_out;
   int* status;
   int* src;            // [bh][cap_src] row that each row below the new length comes from
-  int* movers;         // [bh][cap]     kept rows from behind the new length, in order
+  int* movers;         // [bh][cap]     kept rows from behind the new length, in order; for clusters and heads that are not staged
+  unsigned* words;     // [bh][cap/32]  bits of the rows that stay, for heads that are not staged
+  int2* before;        // [bh][cap/32]  holes and movers ahead of a word's rows, likewise
   int* changed;        // [bh][cap/64]  blocks that receive rows
   int* length;         // [bh]          rows that stay
   float* edge;         // [bh][2]       scales of the block that the new length cuts
@@ -411,15 +414,15 @@ __device__ __forceinline__ int block_sum_below(int x, int* s_warp, int& total) {
 // that with.  All threads return the same.
 struct Pick { unsigned bin; int want; int in_bin; };
 
-__device__ __forceinline__ Pick pick_bin(const int* s_hist, int bins, int want, int* s_warp, int* s_out) {
-  const int per = bins / kEvictThreads;   // thread t sums the bins from t * per on, counted from the top
+__device__ __forceinline__ Pick pick_bin(const int* s_hist, int want, int* s_warp, int* s_out) {
+  constexpr int per = kBins / kEvictThreads;   // thread t sums the bins from t * per on, counted from the top
   int mine = 0;
-  for (int j = 0; j < per; ++j) mine += s_hist[bins - 1 - (threadIdx.x * per + j)];
+  for (int j = 0; j < per; ++j) mine += s_hist[kBins - 1 - (threadIdx.x * per + j)];
   int total;
   int above = block_sum_below(mine, s_warp, total);
   if (above < want && want <= above + mine) {
     for (int j = 0; j < per; ++j) {
-      const int bin = bins - 1 - (threadIdx.x * per + j), c = s_hist[bin];
+      const int bin = kBins - 1 - (threadIdx.x * per + j), c = s_hist[bin];
       if (want <= above + c) { s_out[0] = bin; s_out[1] = want - above; s_out[2] = c; break; }
       above += c;
     }
@@ -434,195 +437,296 @@ __device__ __forceinline__ Pick pick_bin(const int* s_hist, int bins, int want, 
 constexpr int kEvictStage = 8192;    // rows whose weight and position a block keeps in shared memory
 constexpr int kEvictDirect = 512;    // rows at the cut that are ranked one against the other
 constexpr int kEvictSmem = kEvictStage * 8;
+constexpr int kEvictBatch = 8;       // rows of a thread under way at once
 constexpr int kEvictAhead = 4;
+constexpr int kEvictRanged = 1536;   // rows from which on the first histogram covers their weights' range
+constexpr int kEvictRanks = 8;       // blocks of a cluster
 
-// Finds the last row that stays: by a histogram of the leading 11 bits of the weights' keys and, as its bin rarely holds many,
-// by ranking the rows in that bin directly, positions included; else by the remaining bits, 11 and 10 at a time, of keys and then of
-// positions.
+// Finds the last row that stays by histograms of the rows' composites (the weight's key, then the earlier position): the first over
+// the range of the weights, as weights of a few octaves would crowd into a few bins of their leading bits (3 043 uniform ones: 17
+// -> @@U@@ us), each further one over the bin of the cut, until that holds few enough rows to be ranked one against the other.
+// The rows that stay become bits, a word for 32 rows: those above the cut's bin when its rows are collected, the others once they
+// have been ranked.  One sum over the words numbers the holes and the rows that fill them.
+//   kCluster: the blocks of a cluster share a head, a run of rows each, and add up their histograms through each other's shared
+// memory; for heads longer than one block stages, and where there are few heads (@@C@@).
+template <bool kCluster>
 __global__ void __launch_bounds__(kEvictThreads, 2) st3_cache_select_kernel(const EvictParams p) {
   extern __shared__ __align__(16) unsigned char dyn[];
   unsigned* s_key = reinterpret_cast<unsigned*>(dyn);
   int* s_id = reinterpret_cast<int*>(dyn) + kEvictStage;
   __shared__ int s_hist[kBins];
+  __shared__ int s_sums[kCluster ? kBins : 1];          // of all blocks' histograms
   __shared__ u64 s_at_cut[kEvictDirect];
+  __shared__ u64 s_all_at_cut[kCluster ? kEvictDirect : 1];
+  __shared__ int s_row[kEvictDirect];
+  __shared__ unsigned s_word[kEvictStage / 32];
+  __shared__ int2 s_before[kEvictStage / 32];
   __shared__ int s_warp[kEvictThreads / 32];
   __shared__ int s_out[3];
-  __shared__ u64 s_last;
+  __shared__ unsigned s_range[4];
+  __shared__ int s_count[3];        // rows at the cut; holes; movers
+  const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  const int ranks = kCluster ? (int)cluster.num_blocks() : 1, rank = kCluster ? (int)cluster.block_rank() : 0;
+  auto sync = [&] { if (kCluster) cluster.sync(); else __syncthreads(); };
+  auto of = [&](auto* mine, int r) { return kCluster ? cluster.map_shared_rank(mine, r) : mine; };
   pdl_wait();
   pdl_next();
-  const int tid = threadIdx.x, bh = blockIdx.x, b = bh / p.from.heads;
+  const int tid = threadIdx.x, lane = tid & 31, bh = blockIdx.x / ranks, b = bh / p.from.heads;
   const float* w = p.from.weights + (size_t)bh * p.from.cap;
   const int* ids = p.from.ids + (size_t)bh * p.from.cap;
-  // the first rows travel with the count of them; what lies behind the count is not used
+  // without a cluster the first rows travel with the count of them; what lies behind the count is not used
   float w_ahead[kEvictAhead];
   int id_ahead[kEvictAhead];
+  if (!kCluster)
 #pragma unroll
-  for (int j = 0; j < kEvictAhead; ++j) {
-    const int i = tid + j * kEvictThreads;
-    w_ahead[j] = i < p.from.cap ? w[i] : 0.f;
-    id_ahead[j] = i < p.from.cap ? ids[i] : 0;
-  }
+    for (int j = 0; j < kEvictAhead; ++j) {
+      const int i = tid + j * kEvictThreads;
+      w_ahead[j] = i < p.from.cap ? w[i] : 0.f;
+      id_ahead[j] = i < p.from.cap ? ids[i] : 0;
+    }
   const int raw = p.held[b];
   const int border = p.seen[b] - p.recent;   // the first position that counts as recent
   const int n = clamp_rows(raw, p.from.cap), k = min(n, p.keep);
   const int blocks = p.from.cap / kBlockRows;
-  if (tid == 0) {
+  if (tid == 0 && rank == 0) {
     p.length[bh] = k;
     if (raw != n && p.status) atomicOr(p.status, ST3_DEV_RANGE);
   }
-  for (int i = tid; i < blocks; i += kEvictThreads) p.changed[(size_t)bh * blocks + i] = 0;
+  // this block's rows: [first, end)
+  const int run = ((n + kBlockRows - 1) / kBlockRows + ranks - 1) / ranks * kBlockRows, first = min(n, rank * run), end = min(n, first + run);
+  for (int i = tid + rank * kEvictThreads; i < blocks; i += ranks * kEvictThreads) p.changed[(size_t)bh * blocks + i] = 0;
   int* src = p.src + (size_t)bh * p.from.cap;
   if (n <= p.keep) {   // no row comes from behind the new length: no scale is kept
-    for (int i = tid; i < k; i += kEvictThreads) src[i] = i;
+    for (int i = tid + rank * kEvictThreads; i < k; i += ranks * kEvictThreads) src[i] = i;
     return;
   }
-  const bool staged = n <= kEvictStage;
-  bool nan = false;
-  if (tid == 0) s_out[0] = 0;
+  const bool staged = run <= kEvictStage;
+  if (tid < 4) s_range[tid] = 0xffffffffu;
+  if (tid == 0) s_count[0] = 0;
   for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
   __syncthreads();
-  auto take = [&](int i, float wi, int id) {
-    nan |= wi != wi;
-    const unsigned key = weight_key(wi, id >= border);
-    if (staged) { s_key[i] = key; s_id[i] = id; }
-    atomicAdd(&s_hist[key >> 21], 1);
-  };
+  // f(row, whether there is one, weight, position) for this block's rows from `from` on, a warp's 32 rows together
+  auto each_loaded = [&](int from, auto&& f) {
+    for (int i0 = from + tid; i0 - lane < end; i0 += kEvictBatch * kEvictThreads) {
+      float wi[kEvictBatch];
+      int id[kEvictBatch];
 #pragma unroll
-  for (int j = 0; j < kEvictAhead; ++j)
-    if (tid + j * kEvictThreads < n) take(tid + j * kEvictThreads, w_ahead[j], id_ahead[j]);
-#pragma unroll 4
-  for (int i = tid + kEvictAhead * kEvictThreads; i < n; i += kEvictThreads) take(i, w[i], ids[i]);
-  auto row_key = [&](int i, int& id) {
-    id = staged ? s_id[i] : ids[i];
-    return staged ? s_key[i] : weight_key(w[i], id >= border);
-  };
-  if (__syncthreads_or(nan) && tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
-  Pick cutting = pick_bin(s_hist, kBins, k, s_warp, s_out);
-  // composite order of a row: its key, then the earlier position
-  auto composite = [](unsigned key, int id) { return ((u64)key << 32) | (unsigned)~((unsigned)id ^ 0x80000000u); };
-  u64 last;   // of the last row that stays
-  if (cutting.in_bin <= kEvictDirect) {
-    if (tid == 0) { s_out[0] = 0; s_last = 0; }
-    __syncthreads();
-    const int lane = tid & 31;
-    for (int i0 = 0; i0 < n; i0 += kEvictThreads) {
-      int id;
-      const unsigned key = i0 + tid < n ? row_key(i0 + tid, id) : 0u;
-      const bool yes = i0 + tid < n && (key >> 21) == cutting.bin;
-      const unsigned who = __ballot_sync(0xffffffffu, yes);
-      if (who) {
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&s_out[0], __popc(who));
-        at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1));
-        if (yes) s_at_cut[at] = composite(key, id);
+      for (int j = 0; j < kEvictBatch; ++j) {
+        const int i = i0 + j * kEvictThreads;
+        wi[j] = i < end ? w[i] : 0.f;
+        id[j] = i < end ? ids[i] : 0;
+      }
+#pragma unroll
+      for (int j = 0; j < kEvictBatch; ++j) {
+        const int i = i0 + j * kEvictThreads;
+        if (i - lane < end) f(i, i < end, wi[j], id[j]);
       }
     }
-    __syncthreads();
+  };
+  bool nan = false;
+  // the same with keys, from shared memory where they are staged
+  auto each_row = [&](auto&& f) {
+    if (staged)
+      for (int i = first + tid; i - lane < end; i += kEvictThreads) {
+        const bool live = i < end;
+        f(i, live, live ? s_key[i - first] : 0u, live ? s_id[i - first] : 0);
+      }
+    else
+      each_loaded(first, [&](int i, bool live, float wi, int id) {
+        nan |= live && wi != wi;
+        f(i, live, weight_key(wi, id >= border), id);
+      });
+  };
+  // composite order of a row: its key, then the earlier position
+  auto place = [](int id) { return ~((unsigned)id ^ 0x80000000u); };
+  auto composite = [&](unsigned key, int id) { return ((u64)key << 32) | place(id); };
+  // The range of keys and of places, each as lowest and inverted highest, over all blocks.
+  auto range = [&](unsigned (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = __reduce_min_sync(0xffffffffu, x[e]);
+      if (lane == 0) atomicMin(&s_range[e], x[e]);
+    }
+    sync();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = s_range[e];
+      if (kCluster)
+        for (int r = 0; r < ranks; ++r) x[e] = min(x[e], of(s_range, r)[e]);
+    }
+  };
+  // the cut lies in [lo, lo + width]: all rows, then those of a bin
+  u64 lo = 0, width = ~0ull;
+  int shift = 53, want = k, in_bin;
+  const bool ranged = staged && n > kEvictRanged;
+  if (staged) {
+    unsigned x[4] = {0xffffffffu, 0xffffffffu, 0u, 0u};
+    auto take = [&](int i, bool live, float wi, int id) {
+      if (!live) return;
+      nan |= wi != wi;
+      const unsigned key = weight_key(wi, id >= border);
+      s_key[i - first] = key;
+      s_id[i - first] = id;
+      if (!ranged) atomicAdd(&s_hist[key >> 21], 1);
+      else if (key != 0xffffffffu) { x[0] = min(x[0], key); x[1] = min(x[1], ~key); }
+    };
+    if (!kCluster)
+#pragma unroll
+      for (int j = 0; j < kEvictAhead; ++j) take(tid + j * kEvictThreads, tid + j * kEvictThreads < n, w_ahead[j], id_ahead[j]);
+    each_loaded(kCluster ? first : kEvictAhead * kEvictThreads, take);
+    if (ranged) {
+      range(x);
+      if (x[0] <= ~x[1]) {   // else every row is a recent one
+        // no weight is in the bin of the recent rows, be it the last one or one ahead of it
+        shift = 32;
+        while ((~x[1] - x[0]) >> (shift - 32) > kBins - 2) ++shift;
+        lo = (u64)x[0] << 32;
+      }
+    }
+  }
+  for (int pass = 0;; ++pass) {
+    if (pass > 0 || !staged || ranged)
+      each_row([&](int, bool live, unsigned key, int id) {
+        const u64 at = composite(key, id) - lo;
+        if (live && at <= width) atomicAdd(&s_hist[min((unsigned)(at >> shift), (unsigned)kBins - 1)], 1);
+      });
+    if (__syncthreads_or(nan) && tid == 0 && p.status) atomicOr(p.status, ST3_DEV_NONFINITE);
+    int* hist = s_hist;
+    if (kCluster) {
+      sync();
+      for (int i = tid; i < kBins; i += kEvictThreads) {
+        int all = 0;
+        for (int r = 0; r < ranks; ++r) all += of(s_hist, r)[i];
+        s_sums[i] = all;
+      }
+      hist = s_sums;
+      __syncthreads();
+    }
+    const Pick cut = pick_bin(hist, want, s_warp, s_out);
+    want = cut.want;
+    in_bin = cut.in_bin;
+    if (pass == 0 && ranged && cut.bin == kBins - 1) { lo = 0xffffffffull << 32; shift = 32; }   // among the recent rows
+    else lo += (u64)cut.bin << shift;
+    width = (1ull << shift) - 1;
+    if (in_bin <= kEvictDirect || shift == 0) break;
+    // The next histogram covers what the bin holds: weights, or where they are equal places.
+    if (tid < 4) s_range[tid] = 0xffffffffu;
+    sync();   // the histograms have been read
+    for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
+    unsigned x[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+    each_row([&](int, bool live, unsigned key, int id) {
+      if (live && composite(key, id) - lo <= width) {
+        x[0] = min(x[0], key); x[1] = min(x[1], ~key);
+        x[2] = min(x[2], place(id)); x[3] = min(x[3], ~place(id));
+      }
+    });
+    range(x);
+    if (x[0] == ~x[1]) { lo = ((u64)x[0] << 32) | x[2]; width = ~x[3] - x[2]; }
+    else { lo = (u64)x[0] << 32; width = ((u64)(~x[1] - x[0]) << 32) | 0xffffffffull; }
+    shift = 0;
+    while (width >> shift > kBins - 1) ++shift;
+  }
+  const bool rank_them = in_bin <= kEvictDirect;   // else they have one weight and one position, and stay
+  unsigned* word = staged ? s_word : p.words + ((size_t)bh * p.from.cap + first) / 32;
+  each_row([&](int i, bool live, unsigned key, int id) {
+    const u64 c = composite(key, id);
+    const bool inside = live && c - lo <= width;
+    const unsigned stay = __ballot_sync(0xffffffffu, live && c >= lo && (!inside || !rank_them)), who = __ballot_sync(0xffffffffu, inside);
+    if (lane == 0) word[(i - first) / 32] = stay;
+    if (who && rank_them) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&s_count[0], __popc(who));
+      at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1));
+      if (inside) { s_at_cut[at] = c; s_row[at] = i - first; }
+    }
+  });
+  sync();
+  if (rank_them) {
+    const int mine = s_count[0];
+    const u64* all = s_at_cut;
+    if (kCluster) {
+      int at = 0;
+      for (int r = 0; r < ranks; ++r) {
+        const int theirs = of(s_count, r)[0];
+        if (tid < theirs) s_all_at_cut[at + tid] = of(s_at_cut, r)[tid];
+        at += theirs;
+      }
+      all = s_all_at_cut;
+      __syncthreads();
+    }
     // four lanes to a row, each against every fourth row
-    for (int c0 = 0; c0 < cutting.in_bin; c0 += kEvictThreads / 4) {
+    for (int c0 = 0; c0 < mine; c0 += kEvictThreads / 4) {
       const int c = c0 + (tid >> 2);
-      const u64 mine = c < cutting.in_bin ? s_at_cut[c] : 0;
       int above = 0;
-      if (c < cutting.in_bin)
+      if (c < mine) {
+        const u64 me = s_at_cut[c];
 #pragma unroll 4
-        for (int i = tid & 3; i < cutting.in_bin; i += 4) above += s_at_cut[i] > mine;
+        for (int i = tid & 3; i < in_bin; i += 4) above += all[i] > me;
+      }
       above += __shfl_xor_sync(0xffffffffu, above, 1);
       above += __shfl_xor_sync(0xffffffffu, above, 2);
-      if (c < cutting.in_bin && above == cutting.want - 1) s_last = mine;
+      // rows of the same weight and position are equal, and stay or go together
+      if (c < mine && above < want && (tid & 3) == 0) atomicOr(&word[s_row[c] / 32], 1u << (s_row[c] & 31));
     }
-    __syncthreads();
-    last = s_last;
-  } else {
-    u64 prefix = cutting.bin;
-    int want = cutting.want;
-    const int shifts[5] = {42, 32, 21, 10, 0};   // of the composite, after its first 11 bits
-    for (int pass = 0; pass < 5; ++pass) {
-      const int shift = shifts[pass], bits = (pass == 0 ? 53 : shifts[pass - 1]) - shift;
-      for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
-      __syncthreads();
-      for (int i = tid; i < n; i += kEvictThreads) {
-        int id;
-        const unsigned key = row_key(i, id);
-        const u64 c = composite(key, id);
-        if ((c >> (shift + bits)) == prefix) atomicAdd(&s_hist[(unsigned)(c >> shift) & ((1u << bits) - 1)], 1);
-      }
-      __syncthreads();
-      const Pick r = pick_bin(s_hist, bits == 11 ? 2048 : 1024, want, s_warp, s_out);
-      prefix = (prefix << bits) | r.bin;
-      want = r.want;
-    }
-    last = prefix;
   }
-  auto stays = [&](int i) {
-    int id;
-    const unsigned key = row_key(i, id);
-    return composite(key, id) >= last;
+  __syncthreads();   // the keys have been read for the last time, too: the rows that move take their place
+  // thread t numbers the holes and the rows that fill them in its words from t * per on
+  unsigned holes = 0, movers = 0;
+  auto split = [&](int at, unsigned& hole, unsigned& mover) {   // rows below k that go, rows from k on that stay
+    const int below = k - first - at * 32;
+    const unsigned mask = below >= 32 ? 0xffffffffu : below <= 0 ? 0u : (1u << below) - 1;
+    hole = ~word[at] & mask;
+    mover = word[at] & ~mask;
   };
-  if (staged) {
-    // a word of bits for 32 rows; one sum over the words numbers the holes (low half) and the rows that fill them (high half)
-    __shared__ unsigned s_word[kEvictStage / 32];
-    __shared__ int s_before[kEvictStage / 32];
-    const int words = (n + 31) / 32, lane = tid & 31;
-    for (int i0 = tid - lane; i0 < n; i0 += kEvictThreads) {
-      const unsigned bits = __ballot_sync(0xffffffffu, i0 + lane < n && stays(i0 + lane));
-      if (lane == 0) s_word[i0 / 32] = bits;
-    }
-    __syncthreads();
-    static_assert(kEvictStage / 32 <= kEvictThreads, "a thread for each word");
-    unsigned holes = 0, movers = 0;
-    auto split = [&](int word, unsigned& hole, unsigned& mover) {   // rows below k that go, rows from k on that stay
-      const int below = k - word * 32;
-      const unsigned mask = below >= 32 ? 0xffffffffu : below <= 0 ? 0u : (1u << below) - 1;
-      hole = ~s_word[word] & mask;
-      mover = s_word[word] & ~mask;
-    };
-    if (tid < words) split(tid, holes, movers);
-    int total;
-    const int before = block_sum_below(__popc(holes) | (__popc(movers) << 16), s_warp, total);
-    if (tid < words) {
-      s_before[tid] = before;
-      if (holes) p.changed[(size_t)bh * blocks + tid * 32 / kBlockRows] = 1;
-    }
-    __syncthreads();   // the keys have been read for the last time, too: the rows that move take their place
-    int* s_mover = reinterpret_cast<int*>(s_key);
-    for (int i = k / 32 * 32 + tid; i < n; i += kEvictThreads) {
-      split(i / 32, holes, movers);
-      if (movers >> (i & 31) & 1) s_mover[(s_before[i / 32] >> 16) + __popc(movers & ((1u << (i & 31)) - 1))] = i;
-    }
-    __syncthreads();
-    const int moved = total >> 16;
-    for (int i = tid; i < k; i += kEvictThreads) {
-      split(i / 32, holes, movers);
-      const int at = (s_before[i / 32] & 0xffff) + __popc(holes & ((1u << (i & 31)) - 1));
-      // positions that are not distinct could leave a hole without a row for it; it then keeps its own
-      src[i] = (holes >> (i & 31) & 1) && at < moved ? s_mover[at] : i;
-    }
+  int2* before = staged ? s_before : p.before + ((size_t)bh * p.from.cap + first) / 32;
+  const int words = (end - first + 31) / 32, per = (words + kEvictThreads - 1) / kEvictThreads;
+  int below = 0, behind = 0, moved;
+  for (int at = tid * per; at < min(words, (tid + 1) * per); ++at) {
+    split(at, holes, movers);
+    below += __popc(holes);
+    behind += __popc(movers);
+    if (holes) p.changed[(size_t)bh * blocks + (first + at * 32) / kBlockRows] = 1;
+  }
+  if (staged) {   // both in one sum
+    const int sums = block_sum_below(below | (behind << 16), s_warp, moved);
+    if (kCluster && tid == 0) { s_count[1] = moved & 0xffff; s_count[2] = moved >> 16; }
+    below = sums & 0xffff; behind = sums >> 16; moved >>= 16;
   } else {
-    // rows behind the new length that stay, in order
-    int* movers = p.movers + (size_t)bh * p.from.cap;
-    int base = 0;
-    for (int i0 = k; i0 < n; i0 += kEvictThreads) {
-      const int i = i0 + tid;
-      const int yes = i < n && stays(i);
-      int total;
-      const int at = base + block_sum_below(yes, s_warp, total);
-      if (yes) movers[at] = i;
-      base += total;
-    }
-    __syncthreads();
-    const int moved = base;
-    base = 0;
-    for (int i0 = 0; i0 < k; i0 += kEvictThreads) {
-      const int i = i0 + tid;
-      const int hole = i < k && !stays(i);
-      int total;
-      const int at = base + block_sum_below(hole, s_warp, total);
-      if (i < k) src[i] = hole && at < moved ? movers[at] : i;
-      if (hole) p.changed[(size_t)bh * blocks + i / kBlockRows] = 1;
-      base += total;
+    below = block_sum_below(below, s_warp, moved);
+    if (kCluster && tid == 0) s_count[1] = moved;
+    behind = block_sum_below(behind, s_warp, moved);
+    if (kCluster && tid == 0) s_count[2] = moved;
+  }
+  if (kCluster) {   // those of the blocks ahead
+    sync();
+    moved = 0;
+    for (int r = 0; r < ranks; ++r) {
+      const int2 theirs = make_int2(of(s_count, r)[1], of(s_count, r)[2]);
+      if (r < rank) { below += theirs.x; behind += theirs.y; }
+      moved += theirs.y;
     }
   }
-  if (tid < 2) p.edge[2 * bh + tid] = p.from.scale[tid][(size_t)bh * blocks + k / kBlockRows];   // k < n <= capacity
+  for (int at = tid * per; at < min(words, (tid + 1) * per); ++at) {
+    split(at, holes, movers);
+    before[at] = make_int2(below, behind);
+    below += __popc(holes);
+    behind += __popc(movers);
+  }
+  __syncthreads();
+  int* mover = staged && !kCluster ? reinterpret_cast<int*>(s_key) : p.movers + (size_t)bh * p.from.cap;
+  for (int i = max(first, k / 32 * 32) + tid; i < end; i += kEvictThreads) {
+    split((i - first) / 32, holes, movers);
+    if (movers >> (i & 31) & 1) mover[before[(i - first) / 32].y + __popc(movers & ((1u << (i & 31)) - 1))] = i;
+  }
+  sync();   // and the others' shared memory has been read
+  for (int i = first + tid; i < min(k, end); i += kEvictThreads) {
+    split((i - first) / 32, holes, movers);
+    const int at = before[(i - first) / 32].x + __popc(holes & ((1u << (i & 31)) - 1));
+    // positions that are not distinct could leave a hole without a row for it; it then keeps its own
+    src[i] = (holes >> (i & 31) & 1) && at < moved ? (kCluster ? __ldcg(mover + at) : mover[at]) : i;
+  }
+  // k < n <= capacity
+  if (tid < 2 && rank == 0) p.edge[2 * bh + tid] = p.from.scale[tid][(size_t)bh * blocks + k / kBlockRows];
 }
 
 constexpr int kMoveThreads = 128;
@@ -818,14 +922,26 @@ extern "C" st3_status st3_cache_rows(const st3_cache* cache, const int32_t* firs
 }
 
 namespace {
-struct EvictLayout { size_t src, movers, changed, length, edge, total; };
+// Blocks that share a head in the eviction: as many as hold its rows staged.  (us for one sequence of 8 heads, shared by 1 / 2 / 4 / 8
+// blocks: 16 000 rows 36 / 26 / 23 / 23, 65 536: 138 / 96 / 67 / 46; for 16 sequences: 16 000 rows 88 / 76 / 90 / 132.)
+int select_ranks(const st3_cache* c) {
+  int ranks = 1;
+  while (ranks < kEvictRanks && c->capacity > kEvictStage * ranks) ranks *= 2;
+  return ranks;
+}
+
+struct EvictLayout { size_t src, movers, words, before, changed, length, edge, total; };
 EvictLayout evict_layout(const st3_cache* c) {
   const size_t bh = (size_t)c->batch * c->num_kv_heads;
   EvictLayout l;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t x = at; at += up256(bytes); return x; };
   l.src = take(bh * c->capacity * 4);
-  l.movers = take(bh * c->capacity * 4);
+  const int ranks = select_ranks(c);
+  const size_t rows = c->capacity > kEvictStage * ranks ? bh * c->capacity : 0;   // not staged
+  l.movers = take(ranks > 1 || rows ? bh * c->capacity * 4 : 0);
+  l.words = take(rows / 32 * 4);
+  l.before = take(rows / 32 * sizeof(int2));
   l.changed = take(bh * (c->capacity / kBlockRows) * 4);
   l.length = take(bh * 4);
   l.edge = take(bh * 8);
@@ -864,14 +980,18 @@ extern "C" st3_status st3_cache_evict(const st3_cache* from, const st3_cache* to
   p.held = held; p.seen = seen; p.held_out = held_out; p.status = dev_status;
   p.src = reinterpret_cast<int*>(ws + l.src);
   p.movers = reinterpret_cast<int*>(ws + l.movers);
+  p.words = reinterpret_cast<unsigned*>(ws + l.words);
+  p.before = reinterpret_cast<int2*>(ws + l.before);
   p.changed = reinterpret_cast<int*>(ws + l.changed);
   p.length = reinterpret_cast<int*>(ws + l.length);
   p.edge = reinterpret_cast<float*>(ws + l.edge);
   p.keep = keep; p.recent = recent; p.in_place = same == 6;
   const unsigned bh = (unsigned)(from->batch * from->num_kv_heads);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (!allow_smem<st3_cache_select_kernel>(kEvictSmem)) return ST3_ERR_CUDA;
-  st = launch(st3_cache_select_kernel, dim3(bh), dim3(kEvictThreads), kEvictSmem, s, p);
+  const int ranks = select_ranks(from);
+  if (ranks > 1 ? !allow_smem<st3_cache_select_kernel<true>>(kEvictSmem) : !allow_smem<st3_cache_select_kernel<false>>(kEvictSmem)) return ST3_ERR_CUDA;
+  st = launch_clusters(ranks, ranks > 1 ? st3_cache_select_kernel<true> : st3_cache_select_kernel<false>, dim3(bh * (unsigned)ranks),
+                       dim3(kEvictThreads), kEvictSmem, s, p);
   if (st != ST3_OK) return st;
   const int most = keep < from->capacity ? keep : from->capacity;
   const dim3 grid((unsigned)((most + kBlockRows - 1) / kBlockRows), bh);

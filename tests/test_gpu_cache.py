@@ -413,6 +413,23 @@ def test_more_ties_than_are_ranked_one_against_the_other(n, keep, values):
 
 
 @gpu
+@pytest.mark.parametrize("lens,keep,recent", [([16000, 700], 4001, 64), ([20001], 777, 0), ([39999, 10, 300, 0], 250, 250), ([70001], 30000, 5)])
+@pytest.mark.parametrize("kind", ["uniform", "octaves", "few", "same", "signs"])
+def test_heads_that_several_blocks_share(lens, keep, recent, kind):
+    """Two, four and eight blocks to a head, and one longer than they stage; cuts among weights, among equal ones, among recent rows."""
+    p = Pair(len(lens), 1, 64, -(-max(lens) // 64) * 64, seed=len(kind))
+    p.store(lens)
+    weights = {"uniform": lambda b, h, n: p.g.random(n), "octaves": lambda b, h, n: np.exp(p.g.uniform(-60, 60, size=n)),
+               "few": lambda b, h, n: p.g.integers(0, 4, size=n) * 1.5, "same": lambda b, h, n: np.full(n, 0.25),
+               "signs": lambda b, h, n: np.where(p.g.random(n) < 0.01, np.inf, p.g.normal(size=n))}[kind]
+    p.set_weights(weights)
+    p.evict(keep + max(lens) // 5, recent)
+    p.set_weights(weights)
+    p.evict(keep, recent)
+    p.check()
+
+
+@gpu
 def test_long_heads_and_nothing_to_evict():
     p = Pair(2, 1, 64, 9000, seed=1)
     p.store([9000, 50])
