@@ -442,13 +442,16 @@ constexpr int kEvictAhead = 4;
 constexpr int kEvictRanged = 1536;   // rows from which on the first histogram covers their weights' range
 constexpr int kEvictRanks = 8;       // blocks of a cluster
 
-// Finds the last row that stays by histograms of the rows' composites (the weight's key, then the earlier position): the first over
-// the range of the weights, as weights of a few octaves would crowd into a few bins of their leading bits (3 043 uniform ones: 17
-// -> @@U@@ us), each further one over the bin of the cut, until that holds few enough rows to be ranked one against the other.
+// Finds the last row that stays by histograms of the rows' composites (the weight's key, then the earlier position): the first one
+// over their leading 11 bits or, where there are many rows, over the range of the weights, as weights of a few octaves crowd into a
+// few bins of their leading bits (the whole eviction of 64 heads with 3 043 uniform weights: 28.6 -> 18.5 us; under some 1 500
+// rows the pass that finds the range costs more); each further one over the range of what the cut's bin holds, until these are few
+// enough to be ranked one against the other.
 // The rows that stay become bits, a word for 32 rows: those above the cut's bin when its rows are collected, the others once they
 // have been ranked.  One sum over the words numbers the holes and the rows that fill them.
-//   kCluster: the blocks of a cluster share a head, a run of rows each, and add up their histograms through each other's shared
-// memory; for heads longer than one block stages, and where there are few heads (@@C@@).
+// What bounds it: the round trips and barriers of one block, some 11 us at 1 040 rows of 256 heads, ahead of the moves.
+//   kCluster: the blocks of a cluster share a head that is longer than one of them stages, a run of rows each, and add up their
+// histograms through each other's shared memory.  Beyond what eight stage the rows come from L2 in every pass.
 template <bool kCluster>
 __global__ void __launch_bounds__(kEvictThreads, 2) st3_cache_select_kernel(const EvictParams p) {
   extern __shared__ __align__(16) unsigned char dyn[];
