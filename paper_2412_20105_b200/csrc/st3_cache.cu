@@ -608,9 +608,15 @@ __global__ void __launch_bounds__(kEvictThreads, 2) st3_cache_select_kernel(cons
     const Pick cut = pick_bin(hist, want, s_warp, s_out);
     want = cut.want;
     in_bin = cut.in_bin;
-    if (pass == 0 && ranged && cut.bin == kBins - 1) { lo = 0xffffffffull << 32; shift = 32; }   // among the recent rows
-    else lo += (u64)cut.bin << shift;
-    width = (1ull << shift) - 1;
+    if (pass == 0 && ranged && cut.bin == kBins - 1) {   // among the recent rows
+      lo = 0xffffffffull << 32;
+      shift = 32;
+      width = 0xffffffffull;
+    } else {   // the last bin ends where the range does: rows behind it have been counted
+      const u64 skipped = (u64)cut.bin << shift, rest = width - skipped, all = (1ull << shift) - 1;
+      lo += skipped;
+      width = rest < all ? rest : all;
+    }
     if (in_bin <= kEvictDirect || shift == 0) break;
     // The next histogram covers what the bin holds: weights, or where they are equal places.
     if (tid < 4) s_range[tid] = 0xffffffffu;
@@ -640,17 +646,17 @@ __global__ void __launch_bounds__(kEvictThreads, 2) st3_cache_select_kernel(cons
       int at = 0;
       if (lane == 0) at = atomicAdd(&s_count[0], __popc(who));
       at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1));
-      if (inside) { s_at_cut[at] = c; s_row[at] = i - first; }
+      if (inside && at < kEvictDirect) { s_at_cut[at] = c; s_row[at] = i - first; }   // at < in_bin, if nobody writes the weights meanwhile
     }
   });
   sync();
   if (rank_them) {
-    const int mine = s_count[0];
+    const int mine = min(s_count[0], kEvictDirect);
     const u64* all = s_at_cut;
     if (kCluster) {
       int at = 0;
       for (int r = 0; r < ranks; ++r) {
-        const int theirs = of(s_count, r)[0];
+        const int theirs = min(of(s_count, r)[0], kEvictDirect - at);
         if (tid < theirs) s_all_at_cut[at + tid] = of(s_at_cut, r)[tid];
         at += theirs;
       }

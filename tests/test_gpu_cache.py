@@ -429,6 +429,40 @@ def test_heads_that_several_blocks_share(lens, keep, recent, kind):
     p.check()
 
 
+def _scattered(n, gap, far):
+    g = np.random.default_rng(n + gap)
+    return np.concatenate([np.unique(g.integers(0, n * gap, size=n - 2)), [far - 1, far - 2]])
+
+
+def _at_a_border(rows):
+    """Positions up to 2^30 go into 2048 bins of 2^19: many rows on both sides of a border, and a bin that ends 200 short of it."""
+    g, b = np.random.default_rng(rows), 5 << 19
+    more = b + 300 + g.permutation((1 << 19) - 600)[:rows]
+    return np.concatenate([np.arange(b - 700, b + 200), np.sort(more), [b + (1 << 19) - 201, (1 << 30) - 1]])
+
+
+@gpu
+@pytest.mark.parametrize("ids", [_scattered(4000, 300, 1 << 30), _scattered(20000, 50, 1 << 30), _scattered(20000, 3000, (1 << 31) - 1),
+                                 _at_a_border(900), _at_a_border(9000)], ids=["4000", "20000", "far", "border", "long-border"])
+def test_cuts_among_equal_weights_at_scattered_positions(ids):
+    """All weights are equal, so the earliest positions stay; several histograms follow each other before the cut is found."""
+    build()
+    g, n, far = np.random.default_rng(1), len(ids), int(ids[-1]) + 1
+    cap = -(-n // 64) * 64
+    ids = g.permutation(ids).astype(np.int32)
+    cache, into = B.Cache.empty(1, 1, 64, cap), B.Cache.empty(1, 1, 64, cap)
+    cache.k.zero_(), cache.v.zero_(), cache.k_scale.fill_(1), cache.v_scale.fill_(1)
+    cache.weights.fill_(0.125)
+    cache.ids[0, 0, :n] = torch.from_numpy(ids).cuda()
+    held, seen = _i32([n]), _i32([far])
+    for keep in list(range(1, 40)) + list(range(690, 770)) + [int(x) for x in g.integers(40, n, size=200)]:
+        left = cache.evict(held, seen, keep, into=into)
+        got = into.rows(left, keep)[2][0, 0].cpu().numpy()
+        want = np.concatenate([np.sort(ids[ids >= far]), np.sort(ids[ids < far])])[:keep]     # from `seen` on a row is recent
+        assert int(left[0]) == keep and np.array_equal(np.sort(got), np.sort(want)), keep
+    assert int(cache.status) == 0
+
+
 @gpu
 def test_long_heads_and_nothing_to_evict():
     p = Pair(2, 1, 64, 9000, seed=1)
