@@ -247,16 +247,17 @@ __device__ __forceinline__ void pk_give_up(PkShared& sh, int* status) {
   __syncwarp();
 }
 
-// A barrier of the eight warps of a tile of the weights that tells each of them whether any has failed.
-__device__ __forceinline__ bool pk_any_failed(int tile, bool failed) {
+// A barrier of kWarps warps of the weights that tells each of them whether any has failed.
+template <int kWarps>
+__device__ __forceinline__ bool pk_any_failed(int id, bool failed) {
   uint32_t any;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, %2, 256, p;\n\t"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(any)
-      : "r"((uint32_t)failed), "r"(1 + tile)
+      : "r"((uint32_t)failed), "r"(id), "n"(kWarps * 32)
       : "memory");
   return any != 0;
 }
@@ -825,7 +826,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     uint32_t phase = 0, use = 0;
     bool ok = true;
     // the warps of a tile meet in barriers, so they leave together
-    while (!pk_any_failed(x, !pk_next(sh, slot, phase))) {
+    while (!pk_any_failed<8>(1 + x, !pk_next(sh, slot, phase))) {
       const PkItem& it = sh.item[slot];
       const int begin = it.begin, len = it.len, first = it.first[x], t0 = it.steps[x];
       const int tiles = (len - begin + kPkRows - 1) / kPkRows;
@@ -834,7 +835,6 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
       float sum = 0.f;
-      bool left = false;   // the verdict that ends the loops has been given
       // one step ahead: the load's latency runs under the step before, so nothing may be made of it before then
       const float* lse = p.lse_in + (size_t)it.head[0] * p.group * p.total + it.row;
       auto load_lse = [&](int t, int g) {
@@ -843,15 +843,15 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
       };
       WeightSteps s(t0, p.group, rank, ranks);
       float next = load_lse(s.t, s.g);
-      while (s.t < tiles && ok) {
+      while (s.t < tiles) {
         const int t = s.t, q0 = begin + t * kPkRows + half * 64, valid = len - q0;
         const uint32_t buf = use & 1;
         if (r < 64) s_lse[buf * 64 + r] = -kLog2e * next;
-        if (pk_any_failed(x, !ok)) { ok = false; left = true; break; }
+        if (pk_any_failed<4>(11 + group, !ok)) { ok = false; break; }
         s.next();
         next = load_lse(s.t, s.g);
         ok = pk_wait_warp(&sh.scores[2 * x + buf], (use >> 1) & 1, fail);
-        if (!ok) { *fail = 1; break; }   // told to the others at the next barrier
+        if (!ok) { *fail = 1; continue; }   // told to the others at the next barrier
         ++use;
         tc_fence_after();
         uint32_t v[64];
@@ -878,7 +878,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
       // the second half's sums go to the first half's threads, through the places of the second half's lse
       const int pair_bar = 3 + x * 4 + (warp & 3);
       float* s_sum = s_rows + (2 * x + 1) * 128 + r;
-      if (left || pk_any_failed(x, !ok)) { ok = false; break; }   // all of them have read their lse
+      if (pk_any_failed<8>(1 + x, !ok)) { ok = false; break; }   // all of them have read their lse
       if (half == 1) *s_sum = sum;
       asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
       if (kSplit && half == 0) s_rows[2 * x * 128 + r] = sum + *s_sum;   // in the place of the first half's lse
