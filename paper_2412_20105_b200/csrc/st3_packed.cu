@@ -23,11 +23,13 @@
 
 namespace {
 
-// A block of kWarps warps that own rows and a warpgroup of control warps (one of them idle).  The registers of the launch are
+// A block of kWarps warps that own rows and a warpgroup of control warps (in the attention one of them idle).  The registers of the launch are
 // shared out anew: what the owners of rows get and the control warps keep adds up to them.
 template <int kWarps>
 struct PkRoles {
   static constexpr int kMma = kWarps, kLoader = kWarps + 2, kThreads = (kWarps + 4) * 32;
+  static constexpr int kReaders = kWarps == 16 ? kWarps + 3 : kWarps + 2;   // warps that read items
+  static constexpr int kScores = kWarps == 16 ? 2 : 1;                      // arrivals that complete an S
   // In the attention the control warps are the block's first ones, which the schedulers prefer: its MMAs are issued beside warps that
   // always have something to issue (2 % at 12 000 tokens).  The weights lose 5 % that way.
   static __device__ __forceinline__ int warp() {
@@ -82,6 +84,7 @@ struct PkShared {
   uint64_t taken[4];                    // attention: P is in tensor memory; weights: S has been read
   uint64_t added[2], done[2];           // attention: a P V, and the last one of an item, is complete
   uint64_t ready[2], read[2];           // items
+  uint64_t lse_free[2];                 // weights: a step's lse has been read
   uint64_t next;                        // answer of the queue
   uint4 answer;
   PkItem item[2];
@@ -98,10 +101,11 @@ struct PkLayout {
   static constexpr int kStages = D == 128 ? 7 - 2 * kBuffers : 8;
   static constexpr int kRing = 2 * kBuffers * kTile;
   static constexpr int kShared = kRing + kStages * kTile;
-  static constexpr int kLse = kShared + 768;   // weights: two buffers of 64 sums for each of the four warpgroups
-  static constexpr int kTotal = kLse + (kBuffers == 2 ? 4 * 2 * 64 * 4 : 0);
+  static constexpr int kSums = kShared + 512;  // weights: of a tile's second half of columns, and the lse of two steps
+  static constexpr int kLse = kSums + 2 * kPkRows * 4;
+  static constexpr int kTotal = kBuffers == 2 ? kLse + 2 * kPkRows * 4 : kSums;
 };
-static_assert(sizeof(PkShared) <= 768, "PkShared must fit its slot");
+static_assert(sizeof(PkShared) <= 512, "PkShared must fit its slot");
 static_assert(PkLayout<128, 2>::kTotal <= 227 * 1024 && PkLayout<128, 1>::kTotal <= 227 * 1024, "shared memory");
 
 // Bounded wait that also ends when another role of the block has given up.
@@ -114,6 +118,10 @@ __device__ __forceinline__ bool pk_wait(uint64_t* bar, uint32_t parity, volatile
 }
 __device__ __forceinline__ bool pk_wait_warp(uint64_t* bar, uint32_t parity, volatile int* fail) {
   return __all_sync(0xffffffffu, pk_wait(bar, parity, fail));
+}
+
+__device__ __forceinline__ void mbar_arrive_count(uint64_t* bar, uint32_t count) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
 }
 
 __device__ __forceinline__ void take_next(void* answer, uint64_t* bar) {
@@ -185,8 +193,9 @@ __device__ __forceinline__ bool pk_begin(unsigned char* smem, PkShared& sh, int*
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 2); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.own[i], 1); mbar_init(&sh.own_free[i], 2); }
-    for (int i = 0; i < 4; ++i) { mbar_init(&sh.scores[i], 1); mbar_init(&sh.taken[i], Roles::kMma / 2); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.added[i], 1); mbar_init(&sh.done[i], 1); mbar_init(&sh.ready[i], 1); mbar_init(&sh.read[i], Roles::kMma + 2); }
+    for (int i = 0; i < 4; ++i) { mbar_init(&sh.scores[i], Roles::kScores); mbar_init(&sh.taken[i], Roles::kMma / 2); }
+    for (int i = 0; i < 2; ++i) mbar_init(&sh.lse_free[i], Roles::kMma);
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.added[i], 1); mbar_init(&sh.done[i], 1); mbar_init(&sh.ready[i], 1); mbar_init(&sh.read[i], Roles::kReaders); }
     mbar_init(&sh.next, 1);
     sh.fail = 0;
     mbar_fence_init();
@@ -247,17 +256,16 @@ __device__ __forceinline__ void pk_give_up(PkShared& sh, int* status) {
   __syncwarp();
 }
 
-// A barrier of kWarps warps of the weights that tells each of them whether any has failed.
-template <int kWarps>
-__device__ __forceinline__ bool pk_any_failed(int id, bool failed) {
+// A barrier of the eight warps of a tile of the weights that tells each of them whether any has failed.
+__device__ __forceinline__ bool pk_any_failed(int tile, bool failed) {
   uint32_t any;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, %2, %3, p;\n\t"
+      "barrier.cta.red.or.pred q, %2, 256, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(any)
-      : "r"((uint32_t)failed), "r"(id), "n"(kWarps * 32)
+      : "r"((uint32_t)failed), "r"(1 + tile)
       : "memory");
   return any != 0;
 }
@@ -712,13 +720,51 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
   volatile int* fail = &sh.fail;
   const int rows = 2 * kPkRows;
   const int ranks = kSplit ? cluster_ranks() : 1, rank = kSplit ? cluster_rank() : 0;
-  float* s_rows = reinterpret_cast<float*>(smem + L::kLse);
+  float* s_sums = reinterpret_cast<float*>(smem + L::kSums);
+  float* s_lse = reinterpret_cast<float*>(smem + L::kLse);
 
   // Query tiles start at the first query that counts.  steps[x] is the first of them that key tile x takes part in, and
   // `begin` the number of them in all.
   if (warp >= WeightRoles::kMma) pk_fewer_registers<WeightRoles>();
   if (warp > WeightRoles::kLoader) {
-    // idle
+    // Brings the lse of each step's queries, the same for both tiles: an S^T is complete for its readers once they are there, too.
+    // Two steps ahead of them at most, like the products: an arrival at an S^T's barrier must not meet the use before.
+    int slot = 0, at = 0;
+    uint32_t phase = 0, free = 1, use[2] = {0, 0};
+    PkItem it;
+    bool ok = true;
+    while (ok && pk_item(sh, slot, phase, it)) {
+      const int tiles = (it.len - it.begin + kPkRows - 1) / kPkRows;
+      const float* lse = p.lse_in + (size_t)it.head[0] * p.group * p.total + it.row;
+      WeightSteps s(it.steps[0], p.group, rank, ranks);
+      float next[4];
+      auto request = [&] {   // a step ahead; what it brings for queries past the end is not used
+#pragma unroll
+        for (int j = 0; j < 4; ++j) next[j] = lse[(size_t)s.g * p.total + min(it.begin + s.t * kPkRows + 32 * j + lane, it.len - 1)];
+      };
+      request();
+      while (s.t < tiles) {
+        ok = pk_wait_warp(&sh.lse_free[at], free, fail);
+        if (!ok) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s_lse[at * kPkRows + 32 * j + lane] = -kLog2e * next[j];
+        __syncwarp();
+        const bool both = s.t >= it.steps[1];
+        if (lane == 0) {
+          mbar_arrive_cta(&sh.scores[use[0] & 1]);
+          if (both) mbar_arrive_cta(&sh.scores[2 + (use[1] & 1)]);
+          else mbar_arrive_count(&sh.lse_free[at], 8);   // for the warps of the tile that does not take part
+        }
+        __syncwarp();
+        ++use[0];
+        use[1] += both;
+        at ^= 1;
+        free ^= at == 0;
+        s.next();
+        request();
+      }
+    }
+    if (!ok) *fail = 1;
   } else if (warp == WeightRoles::kLoader) {
     Ring<L::kStages> ring;
     int issued = 0, owned = 0;
@@ -821,37 +867,26 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     const int group = warp >> 2, x = group >> 1, half = group & 1, w32 = (warp & 3) * 32, r = w32 + lane;
     const uint32_t lane_addr = (uint32_t)w32 << 16;
     const float sc = kLog2e * rsqrtf((float)D);
-    float* s_lse = s_rows + group * 128;   // two buffers of this warpgroup's 64 queries
+    int at = 0;   // the step's lse
     int slot = 0;
     uint32_t phase = 0, use = 0;
     bool ok = true;
     // the warps of a tile meet in barriers, so they leave together
-    while (!pk_any_failed<8>(1 + x, !pk_next(sh, slot, phase))) {
+    while (!pk_any_failed(x, !pk_next(sh, slot, phase))) {
       const PkItem& it = sh.item[slot];
       const int begin = it.begin, len = it.len, first = it.first[x], t0 = it.steps[x];
       const int tiles = (len - begin + kPkRows - 1) / kPkRows;
       const int key = first + r;
-      u64 acc[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
       float sum = 0.f;
-      // one step ahead: the load's latency runs under the step before, so nothing may be made of it before then
-      const float* lse = p.lse_in + (size_t)it.head[0] * p.group * p.total + it.row;
-      auto load_lse = [&](int t, int g) {
-        const int q = begin + t * kPkRows + half * 64 + r;
-        return r < 64 && t < tiles && q < len ? lse[(size_t)g * p.total + q] : 0.f;
-      };
-      WeightSteps s(t0, p.group, rank, ranks);
-      float next = load_lse(s.t, s.g);
-      while (s.t < tiles) {
-        const int t = s.t, q0 = begin + t * kPkRows + half * 64, valid = len - q0;
+      for (WeightSteps s(it.steps[0], p.group, rank, ranks); s.t < tiles; s.next()) {
+        const float* lse = s_lse + at * kPkRows + half * 64;
+        uint64_t* lse_free = &sh.lse_free[at];
+        at ^= 1;
+        if (s.t < t0) continue;
+        const int q0 = begin + s.t * kPkRows + half * 64, valid = len - q0;
         const uint32_t buf = use & 1;
-        if (r < 64) s_lse[buf * 64 + r] = -kLog2e * next;
-        if (pk_any_failed<4>(11 + group, !ok)) { ok = false; break; }
-        s.next();
-        next = load_lse(s.t, s.g);
         ok = pk_wait_warp(&sh.scores[2 * x + buf], (use >> 1) & 1, fail);
-        if (!ok) { *fail = 1; continue; }   // told to the others at the next barrier
+        if (!ok) { *fail = 1; break; }
         ++use;
         tc_fence_after();
         uint32_t v[64];
@@ -859,29 +894,30 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cta(&sh.taken[2 * x + buf]);   // the next product may overwrite it
+        u64 acc[4];   // 32-bit sums of 16 terms each
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
 #pragma unroll
         for (int part = 0; part < 2; ++part) {   // 32 queries, of which none, all or some count for this warp's keys
           const int c0 = part * 32, lo = key - q0 - c0, hi = valid - c0;
           const int warp_lo = first + w32 - q0 - c0;   // the warp's first key; its last is 31 further
           if (warp_lo > 31 || hi <= 0) continue;
-          if (warp_lo + 31 <= 0 && hi >= 32) add_weights<false>(v, part, s_lse + buf * 64 + c0, sc, 0, 32, acc);
-          else add_weights<true>(v, part, s_lse + buf * 64 + c0, sc, lo, hi, acc);
+          if (warp_lo + 31 <= 0 && hi >= 32) add_weights<false>(v, part, lse + c0, sc, 0, 32, acc);
+          else add_weights<true>(v, part, lse + c0, sc, lo, hi, acc);
         }
-        if (s.t != t) {   // 32-bit sums of at most 64 * group terms each, added up here
-          sum += (sum2(acc[0]) + sum2(acc[1])) + (sum2(acc[2]) + sum2(acc[3]));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
-        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(lse_free);
+        sum += (sum2(acc[0]) + sum2(acc[1])) + (sum2(acc[2]) + sum2(acc[3]));
       }
       const int seq = it.seq, head = it.head[0];
       pk_release(sh, slot, phase);
-      // the second half's sums go to the first half's threads, through the places of the second half's lse
+      // the second half's sums go to the first half's threads
       const int pair_bar = 3 + x * 4 + (warp & 3);
-      float* s_sum = s_rows + (2 * x + 1) * 128 + r;
-      if (pk_any_failed<8>(1 + x, !ok)) { ok = false; break; }   // all of them have read their lse
+      float* s_sum = s_sums + x * kPkRows + r;
+      if (pk_any_failed(x, !ok)) { ok = false; break; }
       if (half == 1) *s_sum = sum;
       asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
-      if (kSplit && half == 0) s_rows[2 * x * 128 + r] = sum + *s_sum;   // in the place of the first half's lse
+      if (kSplit && half == 0) *s_sum += sum;
       if (!kSplit && half == 0 && key < len) p.weights[((size_t)seq * p.kv_heads + head) * p.capacity + key] = sum + *s_sum;
       asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
     }
@@ -894,7 +930,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     const int x = threadIdx.x >> 7, r = threadIdx.x & 127;
     if (rank == 0 && x < 2 && !it.stop && !*fail && it.first[x] + r < it.len) {
       float sum = 0.f;
-      for (int c = 0; c < ranks; ++c) sum += peer_value(s_rows + 2 * x * 128 + r, c);
+      for (int c = 0; c < ranks; ++c) sum += peer_value(s_sums + x * kPkRows + r, c);
       p.weights[((size_t)it.seq * p.kv_heads + it.head[0]) * p.capacity + it.first[x] + r] = sum;
     }
     __syncwarp();
