@@ -649,8 +649,10 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 //   S^T = K Q^T with the keys as rows: a thread owns a key and adds up its row, so nothing is exchanged and no sum's order
 // changes.  Tensor memory holds two S^T for each of the two key tiles; a product runs while the one before it is read.
 // Queries that do not count (before the window, behind the sequence) are left out of the sums.
-// What bounds it: the exponentials, of which the special-function unit does 16 a clock and the FMA pipe takes a quarter: 1 540
-// cycles for both tiles and 128 queries, of 3 000 measured (77 us for 16 prompts of 690 tokens); the MMAs take 1 030.
+// What bounds it: the exponentials, of which the special-function unit does 16 a clock and the FMA pipe takes a quarter (1 540 cycles
+// for both tiles and 128 queries), beside the products, sums and lse that go with them (1 300 without the exponentials), of 2 350
+// measured at 12 000 tokens (0.71 ms; 70 us for 16 prompts of 690); the MMAs take 1 030.  The lse comes by a warp of its own:
+// with barriers between the warps that read it these stayed in step with each other (0.79 ms, 77 us).
 // ------------------------------------------------------------------------------------------------------------------
 // Adds exp2(s * sc - lse) of 32 queries; kSome: of those in [lo, hi) only, whatever the others are.
 template <bool kSome>
@@ -666,7 +668,7 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[64], int part, c
     split2(a, e[0], e[1]);
     e[0] = fast_exp2(e[0]);
     e[1] = fast_exp2(e[1]);
-    if (c & 4) {   // a quarter of the exponentials on the FMA pipe
+    if (c >= 16) {   // a quarter of the exponentials on the FMA pipe, together (spread out: 2 % slower at 12 000 tokens)
       poly_exp2<5>(b, e[2], e[3]);
     } else {
       split2(b, e[2], e[3]);
@@ -997,9 +999,9 @@ st3_status weights_launch(const CUtensorMap& mq, const CUtensorMap& mk, const Pa
 // keys' with all queries, takes as long as a block needs for them.  Shared by the blocks of a cluster, items become more and
 // shorter; against that stand a block's start (2 us, which the queue hides) and that it is done once for each of the blocks.
 // So: as many as the SMs hold, or up to about three rounds of blocks where an item has steps enough (us, shared by 1 / 2 / 4 / 8
-// blocks; 32 heads on 8, D = 128: 700 tokens 37 / 22 / 14 / 17, 2 500: 121 / 67 / 59 / 81, 4 000: 195 / 104 / 122; 8 heads on 2,
-// D = 64: 700: 36 / 20 / 13 / 9; one head to a group, 32 heads: 700: 13 / 15 / 25).  Clusters of eight fit less well: 16 of
-// them take two rounds.
+// blocks; 32 heads on 8, D = 128: 700 tokens 32 / 19 / 13 / 16, 2 500: 106 / 58 / 51 / 71, 4 000: 173 / 89 / 104 / 137; 8 heads on
+// 2, D = 64: 700: 31 / 18 / 11 / 9; one head to a group, 32 heads: 700: 12 / 14 / 24 / 50).  Clusters of eight fit less well: 16
+// of them take two rounds.
 int weights_split(const PackedParams& d) {
   const long long items = ((long long)d.total / (2 * kPkRows) + d.num_seqs) * d.kv_heads;   // at most
   const int longest = d.total / d.num_seqs + 1, queries = d.window > 0 ? min(d.window, longest) : longest;   // for even lengths
