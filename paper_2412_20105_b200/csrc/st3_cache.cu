@@ -7,7 +7,7 @@
 // rounding, or by none where the scale stays, so that rows which move often do not wear out.
 //
 // Every kernel here may be set up while the launch ahead of it runs (programmatic dependent launch) and waits for it
-// before the first access to memory, in every block.
+// before the first access to memory, in every block (the attention's joining launch reads the row counts ahead of that).
 #include "st3_common.cuh"
 
 #include <cooperative_groups.h>
