@@ -49,6 +49,12 @@ constexpr uint32_t kIdescKeys = kIdescBase | ((kPkKeys >> 3) << 17);   // N = 64
 constexpr uint32_t kIdescScores = kIdescBase | ((128u >> 3) << 17);    // N = 128
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+// log2(e) / sqrt(D), with what the tensor core takes off a score given back: its running sum is cut toward zero after every 16
+// dims, by half a unit in the last place on average, which is 0.36 * 2^-23 of it (mantissas spread evenly over their logarithm).
+// Where scores are large the sum grows evenly up to D / 16 such cuts, so the score loses 0.36 * 2^-23 * (D / 16 + 1) / 2 of
+// itself.  With scores up to 10 the weights were off by 9e-7 (a model of these cuts in 64 bits gives the same), and are by 2.6e-7.
+template <int D>
+constexpr float kScoreScale = (float)(1.4426950408889634 / (D == 128 ? 11.313708498984761 : 8.0) * (1.0 + 0.3607 / 8388608.0 * (D / 16 + 1) / 2));
 
 struct PackedParams {
   const int* cu;
@@ -539,7 +545,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     const int x = warp >> 2, w32 = (warp & 3) * 32, r = w32 + lane;
     const uint32_t lane_addr = (uint32_t)w32 << 16;
     const uint32_t tS = tmem + x * 128 + lane_addr, tO = tmem + 256 + x * 128 + lane_addr;
-    const float sc = kLog2e * rsqrtf((float)D);
+    constexpr float sc = kScoreScale<D>;
     int slot = 0;
     uint32_t phase = 0, use = 0, d_phase = 0;   // use: steps so far
     bool ok = true;
@@ -868,7 +874,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     pk_more_registers<WeightRoles>();
     const int group = warp >> 2, x = group >> 1, half = group & 1, w32 = (warp & 3) * 32, r = w32 + lane;
     const uint32_t lane_addr = (uint32_t)w32 << 16;
-    const float sc = kLog2e * rsqrtf((float)D);
+    constexpr float sc = kScoreScale<D>;
     int at = 0;   // the step's lse
     int slot = 0;
     uint32_t phase = 0, use = 0;
