@@ -15,7 +15,8 @@
 // steps a head: 85 -> 77 us); the attention's, of which a block does many more, lost 2 % that way.
 //
 // Roles: four warps (attention) or eight (weights) own a tile each, a row (= tensor memory lane) per thread, in the weights
-// with half of the columns; two warps issue the MMAs of one tile each; one takes items, decodes them and issues the TMA loads.
+// with half of the columns; two warps issue the MMAs of one tile each; one takes items, decodes them and issues the TMA loads; in the
+// weights one more brings the sums of exponentials.
 // Every wait is bounded, and a wait that runs out ends the block's others.
 #include "st3_common.cuh"
 #include "st3_launch.cuh"
