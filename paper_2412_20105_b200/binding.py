@@ -479,8 +479,7 @@ class Cache:
         t = self.torch
         shape = (self.batch, self.num_kv_heads, num_rows)
         like = self.weights.new_empty
-        both = like((2,) + shape + (self.head_dim,), dtype=dtype or t.bfloat16)
-        k, v = both[0], both[1]
+        k, v = like((2,) + shape + (self.head_dim,), dtype=dtype or t.bfloat16).unbind(0)
         ids, weights = self.ids.new_empty(shape), like(shape)
         st3_cache_rows(self.desc, self._count(first, "first"), self._count(held, "held"), num_rows, k.data_ptr(),
                        v.data_ptr(), _dtype_of(k), ids.data_ptr(), weights.data_ptr(), _stream_of(self._index))
