@@ -397,8 +397,9 @@ class Cache:
     `Cache(k, v, k_scale, v_scale, ids, weights)` wraps existing tensors, `Cache.empty(...)` allocates them.  `status` is
     the device status word that the calls report into.  How many rows each sequence holds is the caller's to keep: an
     int32 tensor [batch] that goes into the calls.  The workspaces are kept between calls (one for each number of query
-    heads, with and without weights, and one for evictions): use a Cache on one stream at a time, and order replays of
-    graphs that hold its calls against them and each other."""
+    heads, with and without weights, and one for evictions): use a Cache on one stream at a time, order replays of
+    graphs that hold its calls against them and each other, and keep it as long as such graphs, or calls on another
+    stream than it was made on, may run."""
 
     def __init__(self, k, v, k_scale, v_scale, ids, weights):
         import torch
