@@ -318,7 +318,8 @@ typedef struct {
  *   lse         dev fp32 [num_heads][total], may be NULL: log sum_j exp(q_i . k_j / sqrt(D)) of every row
  *   dev_status  dev int, may be NULL: ST3_DEV_COPY_TIMEOUT as in st3_prefill_attend, ST3_DEV_RANGE if cu is not what it
  *               should be (the sequences concerned are skipped)
- * A value row that is not finite reaches the rows of its own sequence from up to 127 tokens before it on (their
+ * A score of NaN or +Inf makes its row NaN, lse too; one of -Inf has no weight, and a row that has no others is NaN with an lse of
+ * -Inf.  A value row that is not finite reaches the rows of its own sequence from up to 127 tokens before it on (their
  * probability of 0 times Inf), but no other sequence. */
 st3_status st3_packed_attend(const st3_packed* p, const void* q, const void* k, const void* v, const int32_t* cu,
                              void* out, float* lse, int* dev_status, void* cuda_stream);
@@ -326,7 +327,7 @@ st3_status st3_packed_attend(const st3_packed* p, const void* q, const void* k, 
 /* The attention weight each token of the packed prompts has received: for every sequence s, key/value head g and token j
  *   weights[s][g][j] = sum over the heads of the group and over queries i >= j of exp(q_i . k_j / sqrt(D) - lse_i),
  * over all queries (window = 0) or the last `window` of the sequence.  lse is st3_packed_attend's; only k, q and lse are
- * read (v's and out's strides are ignored).
+ * read (v's and out's strides are ignored).  A score or an lse that is NaN makes the tokens that it counts for NaN.
  *   weights     dev fp32 [num_seqs][num_kv_heads][capacity], e.g. st3_cache.weights; places past a sequence's end are
  *               left as they were.  A sequence longer than capacity sets ST3_DEV_RANGE and is skipped. */
 st3_status st3_packed_weights(const st3_packed* p, const void* q, const void* k, const float* lse, const int32_t* cu,

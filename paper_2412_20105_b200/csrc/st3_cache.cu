@@ -118,11 +118,6 @@ __device__ __forceinline__ void values8(const Raw16<T>& r, int half, float (&f)[
     for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
   }
 }
-__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
-  float d;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-  return d;
-}
 // the largest magnitude; NaN if one of them is
 template <typename T>
 __device__ __forceinline__ float top16(const Raw16<T>& r) {

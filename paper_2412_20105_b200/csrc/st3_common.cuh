@@ -166,6 +166,11 @@ __device__ __forceinline__ void unpack16(const uint4& v, float (&f)[4]) {  // f3
   f[2] = __uint_as_float(v.z);
   f[3] = __uint_as_float(v.w);
 }
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 // Packed pairs of fp32 for fma.rn.f32x2 (two FMAs per issued instruction).
 using u64 = unsigned long long;
 __device__ __forceinline__ u64 pack2(float lo, float hi) {

@@ -357,7 +357,8 @@ __device__ __forceinline__ void pk_settle(PkShared& sh, int issued, int owned) {
 // is the start and the end of an item, some 6 000 cycles of its 17 000.
 // ------------------------------------------------------------------------------------------------------------------
 // exp2(s * sc - ref) of a step's columns, as bf16 pairs in w and added up in `add`.  Whole steps take every fourth pair on the
-// FMA pipe; where columns are masked (-Inf, which have to give 0) the special-function unit does them all.
+// FMA pipe; where columns are masked (-Inf, which have to give 0) the special-function unit does them all.  A score of NaN, or of
+// +Inf, makes the row's sum NaN.
 template <bool kWhole>
 __device__ __forceinline__ void probs(const uint32_t (&v)[64], float sc, float ref, u64 (&add)[2], uint32_t (&w)[32]) {
   const float nrf = ref > -INFINITY ? -ref : 0.f;
@@ -584,7 +585,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
           if (__any_sync(0xffffffffu, away)) {
             const float factor = away ? fast_exp2(ref - mx) : 1.f;   // 0 for the first step
             if (away) ref = mx;
-            l *= factor;
+            l = sum_or_nan(l) * factor;   // here and at the end: a sum only grows otherwise
             if (t > 0) {
               // The P V of the step before must be complete.  Waiting for its parity is enough although this thread has not
               // watched every phase: S is complete, hence the P V issued before it, of two steps ago; and this step's cannot
@@ -620,7 +621,8 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
       const int qi = it.first[x] + r, head = it.head[x], row = it.row + qi;
       const bool live = qi < it.len;
       pk_release(sh, slot, phase);
-      const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a sum that is NaN comes through
+      l = sum_or_nan(l);
+      const float inv = ref > -INFINITY ? 1.f / l : NAN;   // NaN where every score is -Inf, and where the sum is NaN
       if (live && p.lse) p.lse[(size_t)head * p.total + row] = ref * kLn2 + logf(l);
       __nv_bfloat16* orow = static_cast<__nv_bfloat16*>(p.out) + (long long)row * p.out_token_stride + (long long)head * p.out_head_stride;
 #pragma unroll 1
@@ -924,6 +926,7 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
       const int pair_bar = 3 + x * 4 + (warp & 3);
       float* s_sum = s_sums + x * kPkRows + r;
       if (pk_any_failed(x, !ok)) { ok = false; break; }
+      sum = sum_or_nan(sum);
       if (half == 1) *s_sum = sum;
       asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
       if (kSplit && half == 0) *s_sum += sum;

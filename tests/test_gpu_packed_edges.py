@@ -1,0 +1,100 @@
+"""Packed prompts where numbers run out: scores that are not finite, values near the end of their range, scores that the tensor
+cores add up exactly, and calls at the edge of what the header allows."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as O
+from paper_2412_20105_b200 import binding as B
+from paper_2412_20105_b200.build import build
+from test_gpu_packed import INVALID, _attend, _check_attend, _desc, _f64, _i32, _inputs, _starts
+
+gpu = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------------------- scores that are not finite
+@gpu
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("bad", ["nan key", "inf score"])
+def test_one_bad_key_reaches_every_later_row_wherever_it_stands(dim, bad):
+    """A NaN score, or one of +Inf, makes its row NaN; rows ahead of the key keep their bits."""
+    lens = [420]
+    q, k, v = _inputs(lens, 2, 1, dim, layout="dense", seed=dim)
+    q[..., 1] = q[..., 1].abs() + 1
+    clean, lse = _attend(q, k, v, lens)
+    for at in list(range(34)) + [63, 64, 100, 127, 128, 133, 255, 300]:
+        k2 = k.clone()
+        if bad == "nan key":
+            k2[at] = float("nan")
+        else:
+            k2[at, 0, 1] = float("inf")
+        out, sums = _attend(q, k2, v, lens)
+        assert torch.equal(out[:at], clean[:at]) and torch.equal(sums[:, :at], lse[:, :at]), at
+        assert torch.isnan(out[at:]).all() and torch.isnan(sums[:, at:]).all(), at
+
+
+@gpu
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("first,last", [(0, 1), (3, 6), (36, 46), (100, 101), (0, 64), (0, 200)])
+def test_scores_of_minus_infinity_have_no_weight(dim, first, last):
+    """Keys first .. last - 1 score -Inf.  A row that sees no others has no softmax; the rest come out as without them."""
+    n = 420
+    q, k, v = _inputs([n], 2, 1, dim, layout="dense", seed=dim + first)
+    q[..., 1] = q[..., 1].abs() + 1
+    k[first:last, 0, 1] = float("-inf")
+    out, sums = _attend(q, k, v, [n])
+    none = last if first == 0 else 0
+    assert torch.isnan(out[:none]).all() and bool((sums[:, :none] == -math.inf).all())
+    kn, vn, qn = _f64(k[:, 0]), _f64(v[:, 0]), _f64(q)
+    kn[first:last] = 0.0
+    for i in list(range(none, n, 17)) + [n - 1]:
+        stay = [j for j in range(i + 1) if not first <= j < last]
+        for h in range(2):
+            x = kn[stay] @ qn[i, h] / math.sqrt(dim)
+            p = np.exp(x - x.max())
+            ref, spread = p @ vn[stay] / p.sum(), p @ np.abs(vn[stay]) / p.sum()
+            # as in _check_attend
+            logit = 2.0 ** -20 * (1 + float((np.abs(kn[stay]) @ np.abs(qn[i, h])).max()) / math.sqrt(dim))
+            assert np.all(np.abs(_f64(out[i, h]) - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2 * logit) * spread + 1e-30), (i, h)
+            total = math.log(p.sum()) + x.max()
+            assert abs(float(sums[h, i]) - total) <= 2 * logit + 2.0 ** -23 * abs(total), (i, h)
+
+
+@gpu
+@pytest.mark.parametrize("copies", [1, 40])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_one_bad_query_reaches_every_key_it_sees(copies, dim):
+    """A NaN query has a NaN lse: every key up to it has received NaN, whatever column the query stands in.  One prompt (items
+    shared by blocks) and many (whole items)."""
+    n = 300
+    lens = [n] * copies
+    q, k, v = _inputs(lens, 2, 1, dim, layout="dense", seed=dim)
+    _, lse = _attend(q, k, v, lens)
+    clean = torch.full((copies, 1, 320), -1.0, device="cuda")
+    B.packed_weights(q, k, lse, _starts(lens), clean)
+    for at in list(range(128, 162)) + [0, 22, 127, 255, 256, 282, n - 1]:
+        for kind in ("both", "lse", "query"):
+            q2, lse2, w = q.clone(), lse.clone(), torch.full_like(clean, -1.0)
+            if kind != "lse":
+                q2[at] = float("nan")
+            if kind != "query":
+                lse2[:, at] = float("nan")
+            B.packed_weights(q2, k, lse2, _starts(lens), w)
+            assert torch.isnan(w[0, 0, :at + 1]).all(), (at, kind)
+            assert torch.equal(w[0, 0, at + 1:], clean[0, 0, at + 1:]) and torch.equal(w[1:], clean[1:]), (at, kind)
+
+
+@gpu
+@pytest.mark.parametrize("window", list(range(1, 33)) + [64, 80])
+def test_one_bad_key_has_received_nan(window):
+    """The last key is seen by the last query only, which stands in column window - 1 of its tile."""
+    n = 200
+    q, k, v = _inputs([n], 2, 1, 64, layout="dense", seed=window)
+    _, lse = _attend(q, k, v, [n])
+    k[n - 1] = float("nan")
+    w = torch.full((1, 1, 256), -1.0, device="cuda")
+    B.packed_weights(q, k, lse, _starts([n]), w, window)
+    assert torch.isnan(w[0, 0, n - 1]) and torch.isfinite(w[0, 0, :n - 1]).all() and bool((w[0, 0, n:] == -1).all())
