@@ -26,6 +26,10 @@ constexpr int kCaConsumers = 4;
 constexpr int kCaThreads = (kCaConsumers + 1) * 32;
 constexpr int kCaHeads = 16;           // query heads of one pass over a group's rows; larger groups take several
 constexpr int kCaStart = 2;            // units of a pair beside its blocks (none: 42.7 us, 1: 40.9, 2: 40.1, 3: 40.2 for 32 users)
+// log2 of the largest probability * scale that goes into f16, whose numbers reach 2^16 and have all their bits down to 2^-14: rows
+// that weigh 2^-29 of the heaviest one do, and lighter ones an absolute step of 2^-39 of it.  (From 1 down there would be 2^15
+// less: a row without a value of its own, e^14 above the others, cost the output 1e-3, and e^17.4 all of it.)
+constexpr float kCaTop = 15.f;
 constexpr int kCaMergeThreads = 128;
 // Rows of the second launch's blocks that add weights: one round of loads, or two where blocks are many.
 __host__ __device__ constexpr int ca_chunk(int split) { return split == 4 ? 512 : 1024; }
@@ -334,7 +338,7 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     }
     // m: running maximum of a head's logits, l: sum of exp2(s - m) over this lane's rows; mv: running maximum of
     // s + log2(V scale), which the probabilities that meet V are relative to, so that blocks of any scale share one
-    // accumulator and the largest term is 1.
+    // accumulator and the largest term is 2^kCaTop.
     float m[kTiles][2], mv[kTiles][2], l[kTiles][2];
     float acc[kTiles][kSteps][4];
 #pragma unroll
@@ -434,7 +438,7 @@ st3_cache_attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           l[n][e & 1] += fast_exp2(v[e] - ref[e & 1]);
-          w[e] = fast_exp2(v[e] + vexp - refv[e & 1]);
+          w[e] = fast_exp2(v[e] + vexp - refv[e & 1] + kCaTop);   // the difference is 0 at most, also where logits have no bits below 1
         }
         const uint32_t lo = half_pair(w[0], w[1]), hi = half_pair(w[2], w[3]);
         pf[0][n][0] = transpose8x8(lo);   // head g, rows 2 t and 2 t + 1
@@ -634,7 +638,7 @@ __global__ void __launch_bounds__(kCaMergeThreads) st3_cache_merge_kernel(const 
 #pragma unroll
       for (int e = 0; e < kVec; ++e) o[e] = fmaf(acc[(size_t)c * p.pitch * D + e], f, o[e]);
     }
-    const float inv = fast_exp2(refv - ref) / sum;   // sums relative to 2^refv over a denominator relative to 2^ref
+    const float inv = fast_exp2(refv - ref - kCaTop) / sum;   // sums relative to 2^(refv - kCaTop) over a denominator relative to 2^ref
     if constexpr (kSplit > 1) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) s_acc[warp][lane * kVec + e] = o[e];

@@ -1,0 +1,54 @@
+"""The 8-bit cache where numbers run out, and calls at the edge of what the header allows."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2412_20105_b200 import binding as B
+from paper_2412_20105_b200.build import build
+from test_gpu_cache import INVALID, Pair, _desc, _i32, _starts
+
+gpu = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ rows that weigh little
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gap", [8.0, 10.0, 14.0, 16.0, 17.25, 20.0])
+@pytest.mark.parametrize("noise", [0.0, 0.5])
+def test_rows_behind_sinks_keep_their_share(dtype, gap, noise):
+    """Rows 0, 16, 32 and 48 of every block outweigh the others by e^gap and have no value of their own: the output is what the
+    others give."""
+    lens, group, dim = [300, 64], 4, 64
+    p = Pair(2, 2, dim, 320, dtype, seed=int(gap))
+    sinks = torch.cat([torch.arange(n) % 16 == 0 for n in lens])
+
+    def change(k, v):
+        k.normal_(generator=torch.Generator().manual_seed(1)).mul_(noise)
+        v.normal_(generator=torch.Generator().manual_seed(2)).add_(0.5)
+        k[:, :, 0] = torch.where(sinks, gap, 0.0)[:, None].to(k.dtype)
+        v[sinks] = 0
+
+    p.store(lens, change=change)
+    p.set_weights(lambda b, h, n: np.zeros(n))
+    q = (torch.randn(2, 2 * group, dim, generator=torch.Generator().manual_seed(3)) * noise).to(p.rows(1).dtype)
+    q[..., 0] = math.sqrt(dim)
+    out = torch.full(q.shape, float("nan"), dtype=q.dtype, device="cuda")
+    p.cache.attend(q.cuda(), _i32(lens), out)
+    assert int(p.cache.status) == 0
+    for b in range(2):
+        for h in range(2):
+            o = p.o[b][h]
+            n = len(o)
+            ref, prob, spread, reach = o.attend(q[b, h * group:(h + 1) * group].double().numpy())
+            got = out[b, h * group:(h + 1) * group].double().cpu().numpy()
+            # Logits, exp2 and the output's rounding as in Pair.attend.  A probability times its block's scale is held relative to
+            # 2^-15 of the largest so far, in f16 (one term, half a step 2^-12 of it; in fp32 two, 2^-23) with an absolute half
+            # step of 2^-25 below 2^-14, that is 2^-40 of the largest, which meets codes of up to 127.
+            logit = 2.0 ** -20 * reach + 2.0 ** -20
+            half, step = (2.0 ** -8, 2.0 ** -12) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -23)
+            largest = (prob * np.repeat(o.vs, 64)[:n]).max() * 127
+            bound = half * np.abs(ref) + (step + 2 * logit) * spread + n * 2.0 ** -40 * largest + 1e-30
+            assert np.all(np.abs(got - ref) <= bound), (b, h, float((np.abs(got - ref) / bound).max()))
