@@ -348,8 +348,9 @@ __device__ __forceinline__ void pk_settle(PkShared& sh, int issued, int owned) {
 // Causal attention, in steps of 64 keys, two to a tile that comes through the ring.
 //   S = Q K^T (128 x 64, D/16 MMAs of K = 16), P = exp2(S - ref) as bf16 over the first half of its S, O += P V.
 // The tensor pipe runs S(0) S(1) | PV(0) S(2) | PV(1) S(3) | ... for each tile, so that the softmax of a step runs under the products
-// of the one before it and of the other tile.  `ref` follows a row's maximum only when that has grown by 2^64: bf16 and
-// fp32 have the range for it and lose no bits, and O is then hardly ever rescaled.
+// of the one before it and of the other tile.  `ref` follows a row's maximum only when that has grown by 2^8: bf16 and
+// fp32 lose no bits by it, O is hardly ever rescaled (as rarely as at 2^64, which values beyond 2^63 would make infinite), and
+// values that add up to less than 2^119 over a sequence stay finite.
 // What bounds it at long prompts: the MMAs, of which a 128x128x16 takes 64 cycles but a 128x64x16 49, as long as its operands take to
 // read from shared memory: 2 600 cycles for both tiles and 128 keys at D = 128, of 3 200 measured (12 000 and 3 043 tokens, 32 heads
 // of 128: 0.97 ms alone, 1 290 TFLOP/s).  Scores of 128 keys would cost 64 cycles an MMA but leave tensor memory no second
@@ -581,7 +582,7 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 #pragma unroll
             for (int e = 0; e < 4; ++e) m4[e] = fmax3(m4[e], __uint_as_float(v[c + e]), __uint_as_float(v[c + 4 + e]));
           const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
-          const bool away = mx > ref + 64.f || (ref == -INFINITY && mx > ref);
+          const bool away = mx > ref + 8.f || (ref == -INFINITY && mx > ref);
           if (__any_sync(0xffffffffu, away)) {
             const float factor = away ? fast_exp2(ref - mx) : 1.f;   // 0 for the first step
             if (away) ref = mx;

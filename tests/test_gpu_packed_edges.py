@@ -98,3 +98,18 @@ def test_one_bad_key_has_received_nan(window):
     w = torch.full((1, 1, 256), -1.0, device="cuda")
     B.packed_weights(q, k, lse, _starts([n]), w, window)
     assert torch.isnan(w[0, 0, n - 1]) and torch.isfinite(w[0, 0, :n - 1]).all() and bool((w[0, 0, n:] == -1).all())
+
+
+# ------------------------------------------------------------------------------------------------ the ends of the range
+@gpu
+@pytest.mark.parametrize("dim", [64, 128])
+def test_large_values_behind_scores_that_grow(dim):
+    """Scores rise by 40 (2^57.7 in weight) behind the first keys, and the values that they meet are near 10^20."""
+    n = 400
+    q, k, v = _inputs([n], 2, 1, dim, layout="dense", seed=dim)
+    k *= 0.01
+    q[..., 0], k[..., 0] = 8.0, 0.0
+    k[96:, 0, 0] = 5 * math.sqrt(dim)
+    v *= 1e20
+    out, lse = _attend(q, k, v, [n])
+    _check_attend(q, k, v, [n], out, lse)
