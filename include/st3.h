@@ -370,7 +370,7 @@ st3_status st3_cache_store(const st3_cache* cache, const void* k, const void* v,
 
 /* One query per head over the rows held (Eq. 2, last row), query head h on key/value head h / (num_heads / num_kv_heads).
  * Scores, sums and weights are fp32.  A probability times its block's scale meets the codes of V as one f16 (ST3_BF16) or the sum of
- * two (ST3_F32): at most 2^-12 or 2^-23 of it is lost, or 2^-40 of the largest such product of its head where that is more.
+ * two (ST3_F32): at most 2^-11 or 2^-22 of it is lost, or 2^-40 of the largest such product of its head where that is more.
  *   q, out       dev [batch][num_heads][head_dim], dtype
  *   held         dev int32 [batch], 0 allowed (the output is then 0); above the capacity: ST3_DEV_RANGE, cut to it
  *   weights_out  dev fp32 [batch][num_kv_heads][capacity] or NULL: weights_in plus each held row's probability, summed over the

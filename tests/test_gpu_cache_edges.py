@@ -45,10 +45,11 @@ def test_rows_behind_sinks_keep_their_share(dtype, gap, noise):
             ref, prob, spread, reach = o.attend(q[b, h * group:(h + 1) * group].double().numpy())
             got = out[b, h * group:(h + 1) * group].double().cpu().numpy()
             # Logits, exp2 and the output's rounding as in Pair.attend.  A probability times its block's scale is held relative to
-            # 2^-15 of the largest so far, in f16 (one term, half a step 2^-12 of it; in fp32 two, 2^-23) with an absolute half
-            # step of 2^-25 below 2^-14, that is 2^-40 of the largest, which meets codes of up to 127.
+            # 2^-15 of the largest so far, in f16 (10 bits behind the first: half a step is 2^-11 of one term; in fp32 a second term
+            # takes the rest, 2^-22) with an absolute half step of 2^-25 below 2^-14, that is 2^-40 of the largest, which meets
+            # codes of up to 127.
             logit = 2.0 ** -20 * reach + 2.0 ** -20
-            half, step = (2.0 ** -8, 2.0 ** -12) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -23)
+            half, step = (2.0 ** -8, 2.0 ** -11) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -22)
             largest = (prob * np.repeat(o.vs, 64)[:n]).max() * 127
             bound = half * np.abs(ref) + (step + 2 * logit) * spread + n * 2.0 ** -40 * largest + 1e-30
             assert np.all(np.abs(got - ref) <= bound), (b, h, float((np.abs(got - ref) / bound).max()))
