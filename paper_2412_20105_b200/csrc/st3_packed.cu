@@ -50,12 +50,10 @@ constexpr uint32_t kIdescKeys = kIdescBase | ((kPkKeys >> 3) << 17);   // N = 64
 constexpr uint32_t kIdescScores = kIdescBase | ((128u >> 3) << 17);    // N = 128
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-// log2(e) / sqrt(D), with what the tensor core takes off a score given back: its running sum is cut toward zero after every 16
-// dims, by half a unit in the last place on average, which is 0.36 * 2^-23 of it (mantissas spread evenly over their logarithm).
-// Where scores are large the sum grows evenly up to D / 16 such cuts, so the score loses 0.36 * 2^-23 * (D / 16 + 1) / 2 of
-// itself.  With scores up to 10 the weights were off by 9e-7 (a model of these cuts in 64 bits gives the same), and are by 2.6e-7.
+// log2(e) / sqrt(D).  The tensor core cuts its running sum toward zero after every 16 dims, which takes 1.9e-7 off a score whose 128
+// terms grow it evenly and nothing off one whose sums have few bits: it depends on the inputs, so nothing is given back.
 template <int D>
-constexpr float kScoreScale = (float)(1.4426950408889634 / (D == 128 ? 11.313708498984761 : 8.0) * (1.0 + 0.3607 / 8388608.0 * (D / 16 + 1) / 2));
+constexpr float kScoreScale = (float)(1.4426950408889634 / (D == 128 ? 11.313708498984761 : 8.0));
 
 struct PackedParams {
   const int* cu;

@@ -113,3 +113,24 @@ def test_large_values_behind_scores_that_grow(dim):
     v *= 1e20
     out, lse = _attend(q, k, v, [n])
     _check_attend(q, k, v, [n], out, lse)
+
+
+# --------------------------------------------------------------------------------------------------- sums that are exact
+@gpu
+@pytest.mark.parametrize("dim", [64, 128])
+def test_weights_of_scores_that_the_tensor_core_adds_up_exactly(dim):
+    """All of a score lies in one dim, so its sum is exact, and lse is 0.  Scores near -50 show what multiplies them."""
+    n = 512
+    q, k = (torch.zeros(n, 1, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    build()
+    g = torch.Generator().manual_seed(dim)
+    q[:, 0, 5] = 64.0
+    k[:, 0, 5] = ((torch.rand(n, generator=g) * 0.2 - 1) * (50.0 * math.sqrt(dim) / 64)).bfloat16().cuda()
+    w = torch.zeros(1, 1, n, device="cuda")
+    B.packed_weights(q, k, torch.zeros(1, n, device="cuda"), _i32([0, n]), w, 1)
+    want = np.exp(_f64(k[:, 0, 5]) * 64.0 / math.sqrt(dim))
+    # the exponent of 2 is at most 72.2: log2(e) / sqrt(D) rounded to 32 bits (half a step, 2^-24 of it), one fma (half a step at
+    # 64 .. 128, 2^-18), both times ln 2; exp2 and its sum with zeros 2^-21
+    bound = math.log(2) * (72.2 * 2.0 ** -24 + 2.0 ** -18) + 2.0 ** -21
+    err = _f64(w[0, 0]) / want - 1
+    assert np.abs(err).max() <= bound, (float(np.abs(err).max()), bound)
