@@ -1054,9 +1054,9 @@ extern "C" st3_status st3_packed_weights(const st3_packed* p, const void* q, con
                                          float* weights, int32_t capacity, int32_t window, int* dev_status, void* cuda_stream) {
   const st3_status st = check_packed(p);
   if (st != ST3_OK) return st;
-  if (capacity < 1 || window < 0 || !aligned(cu, 4) || !aligned(weights, 4) || !aligned(lse, 4)) return ST3_ERR_INVALID_ARG;
-  if (p->total == 0 || p->num_seqs == 0) return ST3_OK;
-  if (!aligned(q, 16) || !aligned(k, 16)) return ST3_ERR_INVALID_ARG;
+  if (capacity < 1 || window < 0 || !aligned(cu, 4)) return ST3_ERR_INVALID_ARG;
+  if (p->total == 0 || p->num_seqs == 0) return ST3_OK;   // empty tensors have no address
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(weights, 4) || !aligned(lse, 4)) return ST3_ERR_INVALID_ARG;
   const EncodeTiledFn encode = tensor_map_encoder();
   CUtensorMap mq, mk;
   if (!encode || !packed_map(encode, &mq, q, p->head_dim, p->num_heads, p->total, p->q_token_stride, p->q_head_stride) ||

@@ -134,3 +134,30 @@ def test_weights_of_scores_that_the_tensor_core_adds_up_exactly(dim):
     bound = math.log(2) * (72.2 * 2.0 ** -24 + 2.0 ** -18) + 2.0 ** -21
     err = _f64(w[0, 0]) / want - 1
     assert np.abs(err).max() <= bound, (float(np.abs(err).max()), bound)
+
+
+# --------------------------------------------------------------------------------------------------- calls at the edge
+def test_nothing_to_do_needs_no_pointers():
+    """Empty tensors have the address 0."""
+    build()
+    lib = B.load()
+    for kw in (dict(total=0), dict(num_seqs=0), dict(total=0, num_seqs=0)):
+        d = _desc(**kw)
+        assert lib.st3_packed_weights(C.byref(d), None, None, None, 4096, None, 128, 0, None, None) == 0
+        assert lib.st3_packed_attend(C.byref(d), None, None, None, 4096, None, None, None, None) == 0
+    d = _desc()
+    assert lib.st3_packed_weights(C.byref(d), 4096, 4096, None, 4096, 4096, 128, 0, None, None) == INVALID
+    assert lib.st3_packed_weights(C.byref(d), 4096, 4096, 4096, 4096, None, 128, 0, None, None) == INVALID
+
+
+@gpu
+@pytest.mark.parametrize("total,seqs", [(0, 3), (20, 0), (0, 0)])
+def test_batches_of_no_tokens_or_no_sequences(total, seqs):
+    q, k, v = _inputs([total], 4, 2, 64, layout="dense")
+    cu = _i32([0] * (seqs + 1))
+    out, lse = torch.full_like(q, 3.0), torch.full((4, total), 3.0, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.packed_attend(q, k, v, cu, out, lse, status)
+    w = torch.full((seqs, 2, 64), 3.0, device="cuda")
+    B.packed_weights(q, k, lse, cu, w, 0, status)
+    assert int(status) == 0 and bool((out == 3).all()) and bool((lse == 3).all()) and bool((w == 3).all())
