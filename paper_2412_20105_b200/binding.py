@@ -468,6 +468,8 @@ class Cache:
     def evict(self, held, seen, keep, recent=0, into=None, held_out=None):
         """Cuts every head to `keep` rows, in place or into another Cache; returns the new numbers of rows held."""
         to = self if into is None else into
+        if to._index != self._index:
+            raise ValueError(f"the target is on cuda:{to._index}, the cache on cuda:{self._index}")
         if held_out is None:
             held_out = self.torch.empty_like(held)
         ws, nbytes = self._workspace("evict", lambda: st3_cache_evict_workspace(self.desc))

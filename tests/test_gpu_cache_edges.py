@@ -53,3 +53,16 @@ def test_rows_behind_sinks_keep_their_share(dtype, gap, noise):
             largest = (prob * np.repeat(o.vs, 64)[:n]).max() * 127
             bound = half * np.abs(ref) + (step + 2 * logit) * spread + n * 2.0 ** -40 * largest + 1e-30
             assert np.all(np.abs(got - ref) <= bound), (b, h, float((np.abs(got - ref) / bound).max()))
+
+
+# --------------------------------------------------------------------------------------------------- calls at the edge
+def test_a_target_on_another_device_is_refused():
+    """Ahead of any launch: stand-ins, as there may be one GPU or none."""
+    class Other:
+        _index, desc = 1, _desc()
+
+    cache = object.__new__(B.Cache)
+    cache._index, cache.desc, cache.torch, cache.batch, cache._workspaces = 0, _desc(), torch, 2, {}
+    counts = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="cuda:1"):
+        cache.evict(counts, counts, 8, into=Other())
