@@ -304,8 +304,9 @@ typedef struct {
   int32_t num_kv_heads;
   int32_t head_dim;      /* 64 or 128                                                               */
   int32_t dtype;         /* ST3_BF16                                                                */
-  /* elements from one token to the next and from one head to the next, multiples of 8: [token][head][D],
-   * [head][token][D] and slices of a fused projection are all possible; the D elements lie side by side */
+  /* elements from one token to the next and from one head to the next, multiples of 8 (anything where there is one token or one
+   * head): [token][head][D], [head][token][D] and slices of a fused projection are all possible; the D elements lie side by
+   * side */
   int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
   int64_t out_token_stride, out_head_stride;
 } st3_packed;

@@ -965,15 +965,17 @@ bool packed_map(EncodeTiledFn fn, CUtensorMap* map, const void* base, int dim, i
 }
 
 bool aligned(const void* p, unsigned a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-bool strides_ok(int64_t token, int64_t head) {   // what a tensor map takes: positive multiples of 16 bytes below 2^40
-  return token > 0 && head > 0 && token % 8 == 0 && head % 8 == 0 && token < (1ll << 39) && head < (1ll << 39);
+bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < (1ll << 39); }   // what a tensor map takes: positive multiples of 16 bytes below 2^40
+bool strides_ok(const st3_packed* p, int heads, int64_t token, int64_t head) {   // of one token or one head none is used
+  return (p->total <= 1 || stride_ok(token)) && (heads == 1 || stride_ok(head));
 }
 
 st3_status check_packed(const st3_packed* p) {
   if (!p) return ST3_ERR_INVALID_ARG;
   if (p->num_seqs < 0 || p->total < 0 || p->num_heads < 1 || p->num_kv_heads < 1 || p->num_heads % p->num_kv_heads) return ST3_ERR_INVALID_ARG;
   if (p->dtype != ST3_BF16 || (p->head_dim != 64 && p->head_dim != 128)) return ST3_ERR_UNSUPPORTED;
-  if (!strides_ok(p->q_token_stride, p->q_head_stride) || !strides_ok(p->k_token_stride, p->k_head_stride)) return ST3_ERR_INVALID_ARG;
+  if (!strides_ok(p, p->num_heads, p->q_token_stride, p->q_head_stride) || !strides_ok(p, p->num_kv_heads, p->k_token_stride, p->k_head_stride))
+    return ST3_ERR_INVALID_ARG;
   // items and tokens are numbered with 31 bits
   if (((long long)p->total / kPkRows + 2ll * p->num_seqs) * p->num_heads > 0x7fffffffLL || p->total > 0x7fffff00) return ST3_ERR_UNSUPPORTED;
   return ST3_OK;
@@ -1029,7 +1031,8 @@ extern "C" st3_status st3_packed_attend(const st3_packed* p, const void* q, cons
                                         void* out, float* lse, int* dev_status, void* cuda_stream) {
   const st3_status st = check_packed(p);
   if (st != ST3_OK) return st;
-  if (!strides_ok(p->v_token_stride, p->v_head_stride) || !strides_ok(p->out_token_stride, p->out_head_stride)) return ST3_ERR_INVALID_ARG;
+  if (!strides_ok(p, p->num_kv_heads, p->v_token_stride, p->v_head_stride) || !strides_ok(p, p->num_heads, p->out_token_stride, p->out_head_stride))
+    return ST3_ERR_INVALID_ARG;
   if (!aligned(cu, 4) || (lse && !aligned(lse, 4))) return ST3_ERR_INVALID_ARG;
   if (p->total == 0 || p->num_seqs == 0) return ST3_OK;
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16)) return ST3_ERR_INVALID_ARG;
@@ -1042,7 +1045,7 @@ extern "C" st3_status st3_packed_attend(const st3_packed* p, const void* q, cons
   PackedParams d = packed_params(p, cu, dev_status);
   d.out = out; d.lse = lse;
   d.out_token_stride = p->out_token_stride; d.out_head_stride = p->out_head_stride;
-  d.wide_out = aligned(out, 32) && p->out_token_stride % 16 == 0 && p->out_head_stride % 16 == 0;
+  d.wide_out = aligned(out, 32) && (p->total == 1 || p->out_token_stride % 16 == 0) && (p->num_heads == 1 || p->out_head_stride % 16 == 0);
   d.by_heads = d.group % 2 == 0;
   d.pairs = d.by_heads ? d.heads / 2 : d.heads;
   d.items = (d.total / (d.by_heads ? kPkRows : 2 * kPkRows) + d.num_seqs) * d.pairs;

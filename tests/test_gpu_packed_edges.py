@@ -161,3 +161,33 @@ def test_batches_of_no_tokens_or_no_sequences(total, seqs):
     w = torch.full((seqs, 2, 64), 3.0, device="cuda")
     B.packed_weights(q, k, lse, cu, w, 0, status)
     assert int(status) == 0 and bool((out == 3).all()) and bool((lse == 3).all()) and bool((w == 3).all())
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="addresses stand in for tensors")
+@pytest.mark.parametrize("kw", [dict(num_kv_heads=1, k_head_stride=0, v_head_stride=4), dict(total=1, q_token_stride=0, out_token_stride=3),
+                                dict(total=1, k_token_stride=-1, v_token_stride=1),
+                                dict(num_heads=1, num_kv_heads=1, q_head_stride=0, k_head_stride=-5, v_head_stride=1, out_head_stride=2)])
+def test_a_stride_that_is_never_used_may_be_anything(kw):
+    """One head, or one token: what torch calls its stride says nothing.  Without a GPU the call gets as far as the driver."""
+    build()
+    lib, d = B.load(), _desc(**kw)
+    assert lib.st3_packed_attend(C.byref(d), 4096, 4096, 4096, 4096, 4096, None, None, None) != INVALID
+    assert lib.st3_packed_weights(C.byref(d), 4096, 4096, 4096, 4096, 4096, 128, 0, None, None) != INVALID
+
+
+@gpu
+def test_one_head_or_one_token_with_strides_of_any_kind():
+    lens = [70, 30]
+    q, k, v = _inputs(lens, 3, 1, 64, layout="dense")
+    want, lse = _attend(q, k, v, lens)
+    odd = lambda x, token, head: x.as_strided(x.shape, (x.stride(0) if token is None else token, x.stride(1) if head is None else head, 1))
+    out = torch.zeros_like(q)
+    got, sums = _attend(q, odd(k, None, 0), odd(v, None, 5), lens, out=out)
+    assert torch.equal(got, want) and torch.equal(sums, lse)
+    w, w2 = torch.zeros(2, 1, 128, device="cuda"), torch.zeros(2, 1, 128, device="cuda")
+    B.packed_weights(q, k, lse, _starts(lens), w)
+    B.packed_weights(q, odd(k, None, 1), lse, _starts(lens), w2)
+    assert torch.equal(w, w2)
+    one = [x[:1].contiguous() for x in (q, k, v)]
+    got, sums = _attend(odd(one[0], 0, None), odd(one[1], 3, None), odd(one[2], 1, None), [1], out=odd(torch.zeros_like(one[0]), 7, None))
+    assert torch.equal(got, v[:1].expand(1, 3, 64)) and torch.isfinite(sums).all()
