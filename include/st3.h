@@ -357,7 +357,7 @@ typedef struct {
 } st3_cache;
 
 /* Stores the rows cu[s] .. cu[s+1]-1 of k and v (dtype ST3_F32 or ST3_BF16; strides in elements from one token and
- * one head to the next, multiples of 16 bytes, the elements of a head side by side) as rows start[s],
+ * one head to the next, multiples of 16 bytes, or anything where there is one; the elements of a head side by side) as rows start[s],
  * start[s]+1, ... of sequence s, with the positions pos[s], pos[s]+1, ... and weight 0: a prompt, a piece of one, or the
  * new token of a decode step.
  *   total       rows of k and v in all

@@ -880,6 +880,8 @@ extern "C" st3_status st3_cache_store(const st3_cache* cache, const void* k, con
   if (total == 0) return ST3_OK;
   if (!aligned16(k) || !aligned16(v)) return ST3_ERR_INVALID_ARG;
   const int unit = dtype == ST3_BF16 ? 8 : 4;   // elements of 16 bytes
+  if (total == 1) k_token_stride = v_token_stride = 0;   // never used, and whatever the caller's tensors call them
+  if (cache->num_kv_heads == 1) k_head_stride = v_head_stride = 0;
   for (int64_t s : {k_token_stride, k_head_stride, v_token_stride, v_head_stride})
     if (s < 0 || s % unit) return ST3_ERR_INVALID_ARG;
   StoreParams p;

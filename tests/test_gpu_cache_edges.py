@@ -66,3 +66,32 @@ def test_a_target_on_another_device_is_refused():
     counts = torch.zeros(2, dtype=torch.int32)
     with pytest.raises(ValueError, match="cuda:1"):
         cache.evict(counts, counts, 8, into=Other())
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="addresses stand in for tensors")
+def test_strides_of_one_head_may_be_anything():
+    """Without a GPU the call gets as far as the launch."""
+    build()
+    lib, d = B.load(), _desc(num_kv_heads=1)
+
+    def store(kt=128, kh=128, vt=128, vh=128, total=5):
+        return lib.st3_cache_store(C.byref(d), 4096, 4096, 1, kt, kh, vt, vh, 4096, total, None, None, None, None)
+
+    assert store(kh=-3, vh=1) != INVALID and store(kt=-1, vt=5, total=1) != INVALID
+    assert store(kt=4) == INVALID and store(vt=-128) == INVALID
+
+
+@gpu
+def test_one_head_or_one_row_with_strides_of_any_kind():
+    odd = lambda x, token, head: x.as_strided(x.shape, (x.stride(0) if token is None else token, x.stride(1) if head is None else head, 1))
+    for heads, n in ((1, 90), (2, 1)):
+        p, other = Pair(1, heads, 64, 128), B.Cache.empty(1, heads, 64, 128)
+        p.store([n])
+        k, v, _, _ = p.cache.rows(_i32([n]), n)
+        k, v = (x[0].transpose(0, 1).contiguous() for x in (k, v))
+        if heads == 1:
+            k, v = odd(k, None, 7), odd(v, None, 1)
+        else:
+            k, v = odd(k, 3, None), odd(v, 0, None)
+        other.store(k, v, _starts([n]))
+        p.check(other, weights=False)
