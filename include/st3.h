@@ -318,7 +318,8 @@ typedef struct {
  *   out         dev, like q with its own strides
  *   lse         dev fp32 [num_heads][total], may be NULL: log sum_j exp(q_i . k_j / sqrt(D)) of every row
  *   dev_status  dev int, may be NULL: ST3_DEV_COPY_TIMEOUT as in st3_prefill_attend, ST3_DEV_RANGE if cu is not what it
- *               should be (the sequences concerned are skipped)
+ *               should be (sequences that are not inside the tensors or end ahead of their start are skipped; what the
+ *               others get is then undefined)
  * Scores and sums are fp32, a probability meets its value as bf16 (2^-8 of it at most is lost).  Values whose magnitudes add up to
  * less than 2^119 over a sequence do not overflow.
  * A score of NaN or +Inf makes its row NaN, lse too; one of -Inf has no weight, and a row that has no others is NaN with an lse of

@@ -191,3 +191,35 @@ def test_one_head_or_one_token_with_strides_of_any_kind():
     one = [x[:1].contiguous() for x in (q, k, v)]
     got, sums = _attend(odd(one[0], 0, None), odd(one[1], 3, None), odd(one[2], 1, None), [1], out=odd(torch.zeros_like(one[0]), 7, None))
     assert torch.equal(got, v[:1].expand(1, 3, 64)) and torch.isfinite(sums).all()
+
+
+@gpu
+@pytest.mark.parametrize("cu", [[0, 128, 127, 256], [0, 256, 255, 256], [0, 200, 100, 256], [0, 256, 0, 256], [300, 300, 300, 300],
+                                [256, 0, 0, 256], [0, 100, 256, 257], [2 ** 31 - 1, 0, 128, 256]])
+def test_every_kind_of_wrong_offsets_is_reported(cu):
+    """Also where no item falls to the sequence that is wrong."""
+    for heads, kv in ((2, 1), (1, 1)):
+        q, k, v = _inputs([256], heads, kv, 64, layout="dense")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        B.packed_attend(q, k, v, _i32(cu), torch.zeros_like(q), None, status)
+        assert int(status) == B.DEV_RANGE, heads
+        status.zero_()
+        B.packed_weights(q, k, torch.zeros(heads, 256, device="cuda"), _i32(cu), torch.zeros(3, kv, 256, device="cuda"), 0, status)
+        assert int(status) == B.DEV_RANGE, heads
+
+
+@gpu
+def test_one_wrong_sequence_among_thousands_is_reported():
+    q, k, v = _inputs([4000], 2, 1, 64, layout="dense")
+    for b in (0, 31, 32, 1999, 3998):
+        cu = torch.arange(4001, dtype=torch.int32)
+        cu[b + 1] -= 2                             # that sequence has -1 tokens, the next one three
+        if b == 3998:
+            cu[4000] = 4001
+        for weights in (False, True):
+            status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            if weights:
+                B.packed_weights(q, k, torch.zeros(2, 4000, device="cuda"), cu.cuda(), torch.zeros(4000, 1, 64, device="cuda"), 0, status)
+            else:
+                B.packed_attend(q, k, v, cu.cuda(), torch.zeros_like(q), None, status)
+            assert int(status) == B.DEV_RANGE, (b, weights)
