@@ -364,8 +364,8 @@ typedef struct {
  *   total       rows of k and v in all
  *   start       dev int32 [batch]: rows held before the call (NULL: 0)
  *   pos         dev int32 [batch] (NULL: start)
- *   dev_status  dev int, may be NULL.  Rows that would leave the cache or the tensors: ST3_DEV_RANGE, the sequence is
- *               skipped. */
+ *   dev_status  dev int, may be NULL.  Rows that would leave the cache or the tensors, or cu not ascending: ST3_DEV_RANGE, the
+ *               sequence is skipped (and where cu is not ascending, what the others get is undefined). */
 st3_status st3_cache_store(const st3_cache* cache, const void* k, const void* v, int32_t dtype, int64_t k_token_stride,
                            int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int32_t* cu,
                            int32_t total, const int32_t* start, const int32_t* pos, int* dev_status, void* cuda_stream);

@@ -144,6 +144,11 @@ __device__ __forceinline__ float top16(const Raw16<T>& r) {
 }
 __device__ __forceinline__ float finite_or_0(float x) { return fabsf(x) <= 3.4028235e38f ? x : 0.f; }
 
+// Whether rows c0 .. c1-1 of the tensors can become rows start and on of a sequence.
+__device__ __forceinline__ bool store_ok(const StoreParams& p, int c0, int c1, int start) {
+  return c0 >= 0 && c1 >= c0 && c1 <= p.total && start >= 0 && start <= p.c.cap - (c1 - c0);
+}
+
 // The sequences' pieces are numbered so that no table is needed: sequence s has the numbers cu[s]/64 + 2 s and on, which are
 // at least as many as the blocks that its rows touch wherever they start (n/64 + 2).
 template <typename T, int D>
@@ -160,6 +165,8 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
   int found = -1, c0 = 0, c1 = 0, start = 0, pos = 0;
   for (int b = tid; b < p.c.batch; b += kStoreThreads) {
     const int from = p.cu[b], to = p.cu[b + 1], st = p.start ? p.start[b] : 0, ps = p.pos ? p.pos[b] : st;
+    // the first block reports for all sequences: one that ends ahead of its start may have no number
+    if (slot == 0 && head == 0 && from != to && !store_ok(p, from, to, st) && p.status) atomicOr(p.status, ST3_DEV_RANGE);
     if (from / kBlockRows + 2 * b <= slot && (b + 1 == p.c.batch || to / kBlockRows + 2 * (b + 1) > slot)) {
       found = b; c0 = from; c1 = to; start = st; pos = ps;
     }
@@ -172,11 +179,7 @@ __global__ void __launch_bounds__(kStoreThreads) st3_cache_store_kernel(const St
   __syncthreads();
   c0 = s_of[0]; c1 = s_of[1]; start = s_of[2]; pos = s_of[3];
   const int n = c1 - c0;
-  if (n == 0) return;
-  if (n < 0 || c0 < 0 || c1 > p.total || start < 0 || start > p.c.cap - n) {   // reported, nothing stored
-    if (tid == 0 && p.status) atomicOr(p.status, ST3_DEV_RANGE);
-    return;
-  }
+  if (n == 0 || !store_ok(p, c0, c1, start)) return;
   const int place = slot - (c0 / kBlockRows + 2 * b);
   if (place < 0) return;
   const int blk = start / kBlockRows + place;

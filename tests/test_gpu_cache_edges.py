@@ -95,3 +95,15 @@ def test_one_head_or_one_row_with_strides_of_any_kind():
             k, v = odd(k, 3, None), odd(v, 0, None)
         other.store(k, v, _starts([n]))
         p.check(other, weights=False)
+
+
+@gpu
+@pytest.mark.parametrize("cu,start", [([0, 640, 0, 640], None), ([0, 64, 0, 64], None), ([0, 640, 639, 640], None), ([640, 0, 0, 0], None),
+                                      ([0, 640, 640, 641], None), ([0, 10, 20, 30], [0, 0, 700]), ([0, 0, 0, 10], [0, 700, 0])])
+def test_every_kind_of_wrong_offsets_is_reported(cu, start):
+    """Also where no block falls to the sequence that is wrong, and where a sequence without rows starts beyond the cache."""
+    p = Pair(3, 2, 64, 640)
+    k = torch.randn(640, 2, 64, generator=torch.Generator().manual_seed(0)).bfloat16().cuda()
+    p.cache.store(k, k, _i32(cu), start=None if start is None else _i32(start))
+    empty_beyond = start == [0, 700, 0]
+    assert int(p.cache.status) == (0 if empty_beyond else B.DEV_RANGE)
