@@ -720,12 +720,15 @@ __device__ __forceinline__ int cluster_ranks() { int r; asm volatile("mov.u32 %0
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float peer_value(const float* mine, int rank) {
-  float x;
-  uint32_t at;
+template <typename T>
+__device__ __forceinline__ T peer_value(const T* mine, int rank) {
+  static_assert(sizeof(T) == 4, "one word");
+  uint32_t at, x;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
-  return x;
+  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  T value;
+  memcpy(&value, &x, 4);
+  return value;
 }
 
 // kSplit: an item belongs to the blocks of a cluster, which share out its steps and have no other item.  The sums are
@@ -953,10 +956,14 @@ st3_packed_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     cluster_sync();
     const PkItem& it = sh.item[0];
     const int x = threadIdx.x >> 7, r = threadIdx.x & 127;
-    if (rank == 0 && x < 2 && !it.stop && !*fail && it.first[x] + r < it.len) {
+    if (rank == 0 && x < 2 && !it.stop && it.first[x] + r < it.len) {
       float sum = 0.f;
-      for (int c = 0; c < ranks; ++c) sum += peer_value(s_sums + x * kPkRows + r, c);
-      p.weights[((size_t)it.seq * p.kv_heads + it.head[0]) * p.capacity + it.first[x] + r] = sum;
+      int failed = 0;   // in any of the blocks: its share of the sums is not there
+      for (int c = 0; c < ranks; ++c) {
+        sum += peer_value(s_sums + x * kPkRows + r, c);
+        failed |= peer_value(&sh.fail, c);
+      }
+      if (!failed) p.weights[((size_t)it.seq * p.kv_heads + it.head[0]) * p.capacity + it.first[x] + r] = sum;
     }
     __syncwarp();
     cluster_sync();   // the others' shared memory stays until it has been read
