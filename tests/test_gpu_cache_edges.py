@@ -107,3 +107,16 @@ def test_every_kind_of_wrong_offsets_is_reported(cu, start):
     p.cache.store(k, k, _i32(cu), start=None if start is None else _i32(start))
     empty_beyond = start == [0, 700, 0]
     assert int(p.cache.status) == (0 if empty_beyond else B.DEV_RANGE)
+
+
+def test_streams_are_found_without_what_torch_may_not_offer(monkeypatch):
+    class Stream:
+        cuda_stream = 1234
+
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.delattr(torch._C, "_cuda_getDevice", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda index: Stream if index == 3 else None)
+    assert B._stream_of(3) == 1234
+    with pytest.raises(ValueError, match="cuda:2"):
+        B._stream_of(2)
