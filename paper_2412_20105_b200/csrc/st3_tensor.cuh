@@ -148,8 +148,8 @@ __device__ __forceinline__ u64 add2(u64 a, u64 b) {
 // exp2 of a pair on the FMA pipe, for a share of a softmax whose other exponentials keep the special-function unit busy (16 a
 // clock and SM, as many as a D = 128 attention step has in the time of its MMAs).  x = i + f with |f| <= 1/2 by adding and
 // taking away 1.5 * 2^23, whose low bits then hold i; 2^f by a minimax polynomial with p(0) = 1 (least squares, reweighted
-// until the relative error levels: 2.8e-6 at degree 4, 9.2e-8 at degree 5); i goes into the exponent.  Arguments below -126
-// give 2^-126.  NaN does not survive the sum of the bits: it gives the largest finite number, Inf gives NaN, and the caller looks
+// until the relative error levels: 2.8e-6 at degree 4, 9.2e-8 at degree 5); i goes into the exponent.  Arguments are held at
+// -127, where the exponent's bits and those of p(0) are all 0: what is below gives 0.  NaN does not survive the sum of the bits: it gives the largest finite number, Inf gives NaN, and the caller looks
 // at its sum by sum_or_nan (2^i by a product of its own would keep NaN: weights received 7 % slower, attention 1 to 3 %).
 template <int kDegree>
 __device__ __forceinline__ void poly_exp2(u64 x, float& ra, float& rb) {
@@ -158,7 +158,7 @@ __device__ __forceinline__ void poly_exp2(u64 x, float& ra, float& rb) {
   constexpr float c5[5] = {0.6931470036506653f, 0.24022242426872253f, 0.05550733581185341f, 0.009671512991189957f, 0.001326472731307149f};
   float a, b;
   split2(x, a, b);
-  x = pack2(max_nan(a, -126.f), max_nan(b, -126.f));
+  x = pack2(max_nan(a, -127.f), max_nan(b, -127.f));
   const u64 t = add2(x, pack2(12582912.f, 12582912.f));
   const u64 f = mul_add2(add2(t, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), x);
   const float top = kDegree == 4 ? c4[3] : c5[4];

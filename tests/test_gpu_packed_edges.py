@@ -223,3 +223,31 @@ def test_one_wrong_sequence_among_thousands_is_reported():
             else:
                 B.packed_attend(q, k, v, cu.cuda(), torch.zeros_like(q), None, status)
             assert int(status) == B.DEV_RANGE, (b, weights)
+
+
+@gpu
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("score", [-200.0, float("-inf")])
+def test_a_score_far_below_leaves_nothing_of_a_large_value(dim, score):
+    """e^-200 times 10^30 is nothing beside values of 10^-10, wherever the key stands."""
+    n = 420
+    q, k, v = _inputs([n], 2, 1, dim, layout="dense", seed=dim)
+    k *= 0.01
+    q[..., 0], k[..., 0] = 8.0, 0.0
+    v *= 1e-10
+    for at in list(range(8)) + [68, 69, 101]:
+        k2, v2 = k.clone(), v.clone()
+        k2[at, 0, 0] = score * math.sqrt(dim) / 8
+        v2[at] = 1e30
+        out, _ = _attend(q, k2, v2, [n])
+        rows = list(range(at + 1, n, 37))
+        qn, kn, vn = _f64(q), _f64(k2[:, 0]), _f64(v2[:, 0])
+        for i in rows:
+            stay = [j for j in range(i + 1) if j != at]
+            for h in range(2):
+                x = kn[stay] @ qn[i, h] / math.sqrt(dim)
+                p = np.exp(x - x.max())
+                want, spread = p @ vn[stay] / p.sum(), p @ np.abs(vn[stay]) / p.sum()
+                logit = 2.0 ** -20 * (1 + float((np.abs(kn[stay]) @ np.abs(qn[i, h])).max()) / math.sqrt(dim))
+                bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2 * logit) * spread + 1e-30
+                assert np.all(np.abs(_f64(out[i, h]) - want) <= bound), (at, i, h)
