@@ -324,6 +324,13 @@ def _stream_of(index: int) -> int:
     return stream(index)
 
 
+def _int32(x, what):
+    """x, which ctypes would cut to its low 32 bits."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{what}: {x} does not fit into 32 bits")
+    return x
+
+
 def _dense(t, shape, dtype, index, what):
     """Address of a dense tensor on CUDA device `index`."""
     if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == index:
@@ -391,7 +398,7 @@ def packed_weights(q, k, lse, cu, weights, window=0, status=None):
     seqs, capacity = cu.numel() - 1, weights.shape[2]
     desc = PackedDesc(seqs, total, heads, kv, dim, _dtype_of(q), *qs, *ks, *ks, *qs)
     st3_packed_weights(desc, qp, kp, _dense(lse, (heads, total), torch.float32, index, "lse"), cup,
-                       _dense(weights, (seqs, kv, capacity), torch.float32, index, "weights"), capacity, window,
+                       _dense(weights, (seqs, kv, capacity), torch.float32, index, "weights"), capacity, _int32(window, "window"),
                        None if status is None else _dense(status, (1,), torch.int32, index, "status"), _stream_of(index))
 
 
@@ -474,6 +481,7 @@ class Cache:
         to = self if into is None else into
         if to._index != self._index:
             raise ValueError(f"the target is on cuda:{to._index}, the cache on cuda:{self._index}")
+        keep, recent = _int32(keep, "keep"), _int32(recent, "recent")
         if held_out is None:
             held_out = self.torch.empty_like(held)
         ws, nbytes = self._workspace("evict", lambda: st3_cache_evict_workspace(self.desc))

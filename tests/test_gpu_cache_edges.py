@@ -120,3 +120,33 @@ def test_streams_are_found_without_what_torch_may_not_offer(monkeypatch):
     assert B._stream_of(3) == 1234
     with pytest.raises(ValueError, match="cuda:2"):
         B._stream_of(2)
+
+
+def test_numbers_beyond_32_bits_are_refused_not_cut():
+    """ctypes would cut 2^32 + 5 to 5."""
+    cache = object.__new__(B.Cache)
+    cache._index, cache.desc, cache.torch, cache.batch, cache.status = 0, _desc(), torch, 2, torch.zeros(1, dtype=torch.int32)
+    counts = torch.zeros(2, dtype=torch.int32)
+    for keep, recent in ((2 ** 32 + 5, 0), (2 ** 31, 1), (8, 2 ** 32), (-2 ** 32 + 8, 0)):
+        with pytest.raises(ValueError, match="32 bits"):
+            cache.evict(counts, counts, keep, recent)
+
+
+@gpu
+def test_a_window_beyond_32_bits_is_refused():
+    build()
+    q, k = torch.zeros(4, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, 1, 64, dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros(1, 1, 64, device="cuda")
+    for window in (2 ** 31, 2 ** 32, 2 ** 32 + 3, -2 ** 32 + 1):
+        with pytest.raises(ValueError, match="32 bits"):
+            B.packed_weights(q, k, torch.zeros(2, 4, device="cuda"), _starts([4]), w, window)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [128, 130, 260])
+def test_groups_beyond_a_pass_of_the_joining_launch(group, dtype):
+    p = Pair(2, 1, 64, 200, dtype, seed=group)
+    p.store([150, 7])
+    p.set_weights(lambda b, h, n: p.g.exponential(size=n))
+    p.attend(group)
