@@ -363,9 +363,10 @@ __device__ __forceinline__ void pk_settle(PkShared& sh, int issued, int owned) {
 // values that add up to less than 2^119 over a sequence stay finite.
 // What bounds it at long prompts: the MMAs, of which a 128x128x16 takes 64 cycles but a 128x64x16 49, as long as its operands take to
 // read from shared memory: 2 600 cycles for both tiles and 128 keys at D = 128, of 3 200 measured (12 000 and 3 043 tokens, 32 heads
-// of 128: 0.97 ms alone, 1 290 TFLOP/s).  Scores of 128 keys would cost 64 cycles an MMA but leave tensor memory no second
-// buffer: a tile's softmax and products then form one chain (3 850 cycles).  At short ones (98 us for 16 prompts of 690 tokens) it
-// is the start and the end of an item, some 6 000 cycles of its 17 000.
+// of 128: 1.00 ms, 1 250 TFLOP/s, in the first 20 ms; 1.17 ms, 1 070 TFLOP/s, in a loop, where the power cap takes the clock to
+// 1 507 MHz).  Scores of 128 keys would cost 64 cycles an MMA but leave tensor memory no second buffer: a tile's softmax and
+// products then form one chain (3 850 cycles).  At short ones (16 prompts of 690 tokens: 101 us, 117 in a loop at 1 597 MHz) it is
+// the start and the end of an item, some 6 000 cycles of its 17 000.
 // ------------------------------------------------------------------------------------------------------------------
 // exp2(s * sc - ref) of a step's columns, as bf16 pairs in w and added up in `add`.  Whole steps take every fourth pair on the
 // FMA pipe; where columns are masked (-Inf, which have to give 0) the special-function unit does them all.  A score of NaN, or of
@@ -672,8 +673,8 @@ st3_packed_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
 // Queries that do not count (before the window, behind the sequence) are left out of the sums.
 // What bounds it: the exponentials, of which the special-function unit does 16 a clock and the FMA pipe takes a quarter (1 540 cycles
 // for both tiles and 128 queries), beside the products, sums and lse that go with them (1 300 without the exponentials), of 2 350
-// measured at 12 000 tokens (0.71 ms; 70 us for 16 prompts of 690); the MMAs take 1 030.  The lse comes by a warp of its own:
-// with barriers between the warps that read it these stayed in step with each other (0.79 ms, 77 us).
+// measured at 12 000 tokens (0.70 ms, in a loop at 1 785 MHz 0.77; 67 and 70 us for 16 prompts of 690); the MMAs take 1 030.  The lse
+// comes by a warp of its own: with barriers between the warps that read it these stayed in step with each other (0.79 ms, 77 us).
 // ------------------------------------------------------------------------------------------------------------------
 // Adds exp2(s * sc - lse) of 32 queries; kSome: of those in [lo, hi) only, whatever the others are.
 template <bool kSome>
