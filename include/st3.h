@@ -335,7 +335,8 @@ st3_status st3_packed_attend(const st3_packed* p, const void* q, const void* k, 
  * over all queries (window = 0) or the last `window` of the sequence.  lse is st3_packed_attend's; only k, q and lse are
  * read (v's and out's strides are ignored).  A score or an lse that is NaN makes the tokens that it counts for NaN.
  *   weights     dev fp32 [num_seqs][num_kv_heads][capacity], e.g. st3_cache.weights (after st3_cache_store, which sets the
- *               weights of the rows it stores to 0); places past a sequence's end are left as they were.  A sequence longer than capacity sets ST3_DEV_RANGE and is skipped. */
+ *               weights of the rows it stores to 0); places past a sequence's end are left as they were.  A sequence longer
+ *               than capacity sets ST3_DEV_RANGE and is skipped. */
 st3_status st3_packed_weights(const st3_packed* p, const void* q, const void* k, const float* lse, const int32_t* cu,
                               float* weights, int32_t capacity, int32_t window, int* dev_status, void* cuda_stream);
 

@@ -149,8 +149,10 @@ __device__ __forceinline__ u64 add2(u64 a, u64 b) {
 // clock and SM, as many as a D = 128 attention step has in the time of its MMAs).  x = i + f with |f| <= 1/2 by adding and
 // taking away 1.5 * 2^23, whose low bits then hold i; 2^f by a minimax polynomial with p(0) = 1 (least squares, reweighted
 // until the relative error levels: 2.8e-6 at degree 4, 9.2e-8 at degree 5); i goes into the exponent.  Arguments are held at
-// -127, where the exponent's bits and those of p(0) are all 0: what is below gives 0.  NaN does not survive the sum of the bits: it gives the largest finite number, Inf gives NaN, and the caller looks
-// at its sum by sum_or_nan (2^i by a product of its own would keep NaN: weights received 7 % slower, attention 1 to 3 %).
+// -127, where the exponent's bits and those of p(0) are all 0: what is below gives 0.
+// NaN does not survive the sum of the bits: it gives the largest finite number (Inf gives NaN), and whoever adds up the results
+// passes the sum through sum_or_nan.  (2^i by a product of its own would keep NaN: weights received 7 % slower, attention 1 to
+// 3 %.)
 template <int kDegree>
 __device__ __forceinline__ void poly_exp2(u64 x, float& ra, float& rb) {
   static_assert(kDegree == 4 || kDegree == 5, "coefficients");
